@@ -454,6 +454,151 @@ int dcp_layer_bwd(const dcp_layer_desc* desc, const dcp_layer_weights* w, const 
                   const dcp_layer_grads* grads, void* stash, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------ */
+/* 8-bit activation checkpoints                                              */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * Formats of a kept activation.  DCP_ACT_INT8 and DCP_ACT_E4M3 hold a bf16
+ * matrix [rows, cols] as one 8-bit code an element (two's complement, or 4
+ * exponent and 3 mantissa bits without infinities) and one scale byte for each
+ * group of 32 consecutive columns of a row: with qmax = 127 or 448, k is the
+ * smallest integer >= -126 with max |x| <= qmax 2^k over the group, the byte is
+ * k + 127, a code x / 2^k rounded to the format (nearest, ties to even), and the
+ * value it stands for code 2^k, exact in bf16 (a value that was rounded up to
+ * 2^128 reads back as infinity).  An element moves by at most half
+ * a step: max |x| of its group / 127 (int8, whose scale wastes less than one
+ * bit), or 2^-4 of itself (e4m3, from 2^-13 of the group's max on).  A group that
+ * holds a NaN or an infinity reads back as NaN (byte 255, codes 0).  Codes are
+ * [rows, cols] and scale bytes [rows, ceil(cols / 32)], both contiguous.
+ */
+enum { DCP_ACT_BF16 = 0, DCP_ACT_INT8 = 1, DCP_ACT_E4M3 = 2 };
+
+/*
+ *   rows    >= 0 (nothing is enqueued for 0), < 2^31.
+ *   cols    a positive multiple of 8; a row's last group may be short.
+ *   ld      row stride of the call's bf16 matrices in elements: a multiple of 8,
+ *           >= cols (a slice of a wider matrix; columns outside are not touched).
+ *   format  DCP_ACT_INT8 or DCP_ACT_E4M3 (DCP_ACT_BF16: dcp_act8_gelu_bwd only).
+ * bf16 and fp32 pointers are 16-byte aligned, codes 8-byte.  The calls only
+ * enqueue one kernel on `stream` (they may be captured into a graph).
+ */
+typedef struct {
+  int64_t rows;
+  int32_t cols;
+  int32_t format;
+  int64_t ld;
+} dcp_act8_desc;
+
+/* codes, scales = checkpoint of x (bf16). */
+int dcp_act8_pack(const dcp_act8_desc* desc, const void* x, void* codes, void* scales, void* stream);
+
+/* x (bf16) = the values that the checkpoint stands for. */
+int dcp_act8_unpack(const dcp_act8_desc* desc, const void* codes, const void* scales, void* x, void* stream);
+
+/*
+ * The activation's backward from the checkpoint of its input u: du = da o
+ * GELU'(u) and a = GELU(u) (tanh form), the left operand of the next weight
+ * gradient, all bf16.  With DCP_ACT_BF16 `codes` is u itself (row stride ld) and
+ * `scales` is not read.  du or a may be da's buffer (or, in bf16, u's).
+ */
+int dcp_act8_gelu_bwd(const dcp_act8_desc* desc, const void* codes, const void* scales, const void* da, void* du,
+                      void* a, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Gated, normed join of a branch into the residual stream                   */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * For row t of a packed batch, with f the output of a block's branch (attention
+ * or MLP), x the residual stream and s the row's sequence:
+ *   n = RMSNorm(f; post),  out = residual_scale x + gate_s o n,
+ *   y = RMSNorm(out; pre)  (the next branch's input, from out in fp32).
+ * Each of the three may be absent: without post n = f, without gate it is 1,
+ * without pre there is no y.
+ *   rows            rows allocated in every matrix, in [0, 2^31).
+ *   hidden          a positive multiple of 8, at most 4096 (DCP_ERR_UNSUPPORTED
+ *                   beyond).
+ *   n_seqs, cu_seqlens  a gate for each sequence: cu_seqlens is int32 [n_seqs+1]
+ *                   in DEVICE memory (cu[0] = 0, non-decreasing, cu[n_seqs] <= rows;
+ *                   empty sequences are allowed), gate is [n_seqs, hidden], and rows
+ *                   from cu[n_seqs] on are neither read for any output nor written.
+ *                   0 and NULL: gate, if any, is one row [hidden] for all rows.
+ *                   The library cannot check values that only the device holds:
+ *                   offsets that break these rules give wrong numbers, never an
+ *                   access outside the buffers.
+ *   residual_scale  finite.
+ *   eps             finite, >= 0.
+ *   keep_format     format in which f and out are kept from forward to backward.
+ *   dy_f32          backward: dy is fp32 (as a product leaves it), else bf16.
+ *   accumulate      backward: 1 adds the gradients of post, gate and pre to what is
+ *                   there, 0 writes them.
+ */
+typedef struct {
+  int64_t rows;
+  int32_t hidden;
+  int32_t n_seqs;
+  const int32_t* cu_seqlens;
+  float residual_scale;
+  float eps;
+  int32_t keep_format;
+  int32_t dy_f32;
+  int32_t accumulate;
+} dcp_gated_norm_desc;
+
+/* bf16 device arrays [hidden], [hidden] or [n_seqs, hidden], [hidden]; NULL where
+ * absent. */
+typedef struct {
+  const void *post, *gate, *pre;
+} dcp_gated_norm_weights;
+
+/* An activation kept in desc->keep_format: bf16 [rows, hidden] and no scales, or
+ * codes and scale bytes (see above). */
+typedef struct {
+  void* data;
+  void* scales;
+} dcp_kept;
+
+/*
+ * Forward.  x, f, out, y bf16 [rows, hidden]; y and rstd_out (fp32 [rows], 1 /
+ * rms(out)) with pre only, rstd_f (1 / rms(f)) with post only, NULL otherwise.
+ * keep_f / keep_out: where to write the 8-bit checkpoint of f and of out (of its
+ * bf16 values); NULL, or data NULL, for none; with DCP_ACT_BF16 both must be none (f
+ * and out are the kept activations).  out may be x's or f's buffer and y f's or, if
+ * it is not out's, x's.
+ */
+int dcp_gated_norm_fwd(const dcp_gated_norm_desc* desc, const dcp_gated_norm_weights* w, const void* x, const void* f,
+                       void* out, void* y, float* rstd_f, float* rstd_out, const dcp_kept* keep_f,
+                       const dcp_kept* keep_out, void* stream);
+
+/* Workspace bytes of the backward (256-byte aligned device memory). */
+int dcp_gated_norm_bwd_workspace_size(const dcp_gated_norm_desc* desc, size_t* bytes);
+
+/* fp32 gradients, one for each weight that is present, of its shape. */
+typedef struct {
+  float *post, *gate, *pre;
+} dcp_gated_norm_grads;
+
+/*
+ * Backward of <dout, out> + <dy, y>, from f and out as kept and the forward's row
+ * scales: dx = residual_scale G and df = RMSNorm'(gate o G) with G the gradient
+ * of out, and the gradients of the weights.  y may be asked for again (the left
+ * operand of the next branch's weight gradient, RMSNorm of out as kept).
+ *   dout  bf16 [rows, hidden], or NULL for zero (only y is used; needs pre).
+ *   dy    bf16 or fp32 [rows, hidden] with pre, NULL without.
+ *   f     needed with post or gate (NULL otherwise); out with pre.
+ *   dx    may be NULL (residual_scale 1 and no pre: it would equal dout).
+ *   y     may be NULL; needs pre.
+ * A gate's gradient is summed over its sequence's rows (0 for an empty one), or
+ * over all rows where one gate serves all.  Sums are fp32, in an order fixed by rows
+ * and hidden: results are bitwise reproducible.  dx or df may be dout's buffer, y, dx
+ * or df a bf16 dy's.  Two calls that overlap in time need two workspaces.
+ */
+int dcp_gated_norm_bwd(const dcp_gated_norm_desc* desc, const dcp_gated_norm_weights* w, const void* dout,
+                       const void* dy, const dcp_kept* f, const dcp_kept* out, const float* rstd_f,
+                       const float* rstd_out, void* dx, void* df, void* y, const dcp_gated_norm_grads* grads,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
 /* Schedule replay: DCP against bucket parallelism (Secs. 2.3-2.4, 4.1-4.2)   */
 /* ------------------------------------------------------------------------ */
 

@@ -12,7 +12,7 @@ import ctypes as C
 import math
 import os
 from dataclasses import dataclass, field
-from typing import List, Optional, Sequence
+from typing import List, NamedTuple, Optional, Sequence, Tuple
 
 import numpy as np
 
@@ -91,6 +91,28 @@ class LayerWeightsC(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("norm1", "wq", "wk", "wv", "wo", "norm2", "w_up", "w_down")]
 
 
+class Act8DescC(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int32), ("format", C.c_int32), ("ld", C.c_int64)]
+
+
+class GatedNormDescC(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("hidden", C.c_int32), ("n_seqs", C.c_int32), ("cu_seqlens", C.c_void_p),
+                ("residual_scale", C.c_float), ("eps", C.c_float), ("keep_format", C.c_int32), ("dy_f32", C.c_int32),
+                ("accumulate", C.c_int32)]
+
+
+class GatedNormPtrsC(C.Structure):
+    _fields_ = [("post", C.c_void_p), ("gate", C.c_void_p), ("pre", C.c_void_p)]
+
+
+class KeptC(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("scales", C.c_void_p)]
+
+
+ACT_BF16, ACT_INT8, ACT_E4M3 = 0, 1, 2
+ACT_FORMATS = {"bf16": ACT_BF16, "int8": ACT_INT8, "e4m3": ACT_E4M3}
+ACT_GROUP = 32  # columns that share a scale byte
+
 LAYER_PARAMS = ("norm1", "wq", "wk", "wv", "wo", "norm2", "w_up", "w_down")
 
 _lib = None
@@ -133,6 +155,14 @@ def load() -> C.CDLL:
         "dcp_layer_fwd": ([C.POINTER(LayerDescC), C.POINTER(LayerWeightsC), vp, vp, vp, vp, sz, vp], C.c_int),
         "dcp_layer_bwd": ([C.POINTER(LayerDescC), C.POINTER(LayerWeightsC), vp, vp, vp, C.POINTER(LayerWeightsC), vp,
                            vp, sz, vp], C.c_int),
+        "dcp_act8_pack": ([C.POINTER(Act8DescC), vp, vp, vp, vp], C.c_int),
+        "dcp_act8_unpack": ([C.POINTER(Act8DescC), vp, vp, vp, vp], C.c_int),
+        "dcp_act8_gelu_bwd": ([C.POINTER(Act8DescC), vp, vp, vp, vp, vp, vp], C.c_int),
+        "dcp_gated_norm_fwd": ([C.POINTER(GatedNormDescC), C.POINTER(GatedNormPtrsC), vp, vp, vp, vp, vp, vp,
+                                C.POINTER(KeptC), C.POINTER(KeptC), vp], C.c_int),
+        "dcp_gated_norm_bwd_workspace_size": ([C.POINTER(GatedNormDescC), C.POINTER(sz)], C.c_int),
+        "dcp_gated_norm_bwd": ([C.POINTER(GatedNormDescC), C.POINTER(GatedNormPtrsC), vp, vp, C.POINTER(KeptC),
+                                C.POINTER(KeptC), vp, vp, vp, vp, vp, C.POINTER(GatedNormPtrsC), vp, sz, vp], C.c_int),
         "dcp_simulate": ([C.POINTER(C.c_int64), C.c_int32, C.POINTER(C.c_int32), C.c_int32, C.POINTER(CostTableC),
                           C.c_int64, C.POINTER(PlanOptsC), C.POINTER(SimOptsC), C.POINTER(SimResultC),
                           C.POINTER(SimResultC)], C.c_int),
@@ -573,3 +603,329 @@ class Layer:
                                       _nbytes(self.ws), self.stream))
         self.stash = None
         return dx
+
+
+# ---------------------------------------------------------------------------
+# 8-bit activation checkpoints
+
+def _on_device(call):
+    """Runs a call's launches with its tensors' device as the current one."""
+    def run(torch, device, *args):
+        if device.index is None or device.index == torch.cuda.current_device():
+            return call(torch, device, *args)
+        with torch.cuda.device(device):
+            return call(torch, device, *args)
+    return run
+
+
+@_on_device
+def _enqueue(torch, device, fn, *args):
+    _check(fn(*args, torch.cuda.current_stream(device).cuda_stream))
+
+
+def _act_dtype(torch, fmt: str):
+    if fmt not in ("int8", "e4m3"):
+        raise ValueError(f"fmt must be 'int8' or 'e4m3', not {fmt!r}")
+    return torch.int8 if fmt == "int8" else torch.float8_e4m3fn
+
+
+def _act_format(torch, codes) -> int:
+    fmt = {torch.int8: ACT_INT8, torch.float8_e4m3fn: ACT_E4M3, torch.bfloat16: ACT_BF16}.get(codes.dtype)
+    if fmt is None:
+        raise ValueError(f"codes must be int8 or float8_e4m3fn, not {codes.dtype}")
+    return fmt
+
+
+def _same_device(ref, name, others):
+    """Everything in ``others`` (name, tensor) is on ref's CUDA device."""
+    if not ref.is_cuda:
+        raise ValueError("tensors must be on a CUDA (HIP) device")
+    for n, t in others:
+        if t.device != ref.device:
+            raise ValueError(f"{n} is on {t.device}, {name} on {ref.device}")
+
+
+def _check_rows(torch, t, name, shape=None):
+    """A bf16 [rows, cols] matrix of contiguous rows; returns its row stride."""
+    if not hasattr(t, "dim") or t.dim() != 2 or t.dtype != torch.bfloat16:
+        raise ValueError(f"{name} must be a bf16 tensor of shape [rows, cols]")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    return int(t.stride(0)) if t.shape[0] > 1 else int(t.shape[1])
+
+
+def _check_codes(torch, codes, scales, shape=None):
+    """A checkpoint: contiguous codes [rows, cols] and their uint8 scale bytes."""
+    if not hasattr(codes, "dim") or codes.dim() != 2 or not codes.is_contiguous():
+        raise ValueError("codes must be a contiguous tensor of shape [rows, cols]")
+    rows, cols = (int(n) for n in codes.shape)
+    if shape is not None and (rows, cols) != tuple(shape):
+        raise ValueError(f"codes have shape {(rows, cols)}, not {tuple(shape)}")
+    want = (rows, -(-cols // ACT_GROUP))
+    if not hasattr(scales, "dim") or tuple(scales.shape) != want or scales.dtype != torch.uint8 \
+            or not scales.is_contiguous():
+        raise ValueError(f"scales must be a contiguous uint8 tensor of shape {want}")
+
+
+def act8_pack(x, fmt: str = "int8", codes=None, scales=None):
+    """The 8-bit checkpoint (codes, scales) of a bf16 [rows, cols] matrix (see
+    dcp_act8_pack): codes int8 or float8_e4m3fn, one scale byte for 32 columns.
+    ``x`` may be a slice of a wider matrix (contiguous rows, a row stride that is
+    a multiple of 8)."""
+    import torch
+    dtype = _act_dtype(torch, fmt)
+    ld = _check_rows(torch, x, "x")
+    rows, cols = (int(n) for n in x.shape)
+    _same_device(x, "x", [(n, t) for n, t in (("codes", codes), ("scales", scales)) if t is not None])
+    codes = torch.empty((rows, cols), dtype=dtype, device=x.device) if codes is None else codes
+    if scales is None:
+        scales = torch.empty((rows, -(-cols // ACT_GROUP)), dtype=torch.uint8, device=x.device)
+    _check_codes(torch, codes, scales, x.shape)
+    if codes.dtype != dtype:
+        raise ValueError(f"codes must be {dtype} for fmt {fmt!r}")
+    d = Act8DescC(rows, cols, ACT_FORMATS[fmt], ld)
+    _enqueue(torch, x.device, load().dcp_act8_pack, d, x.data_ptr(), codes.data_ptr(), scales.data_ptr())
+    return codes, scales
+
+
+def act8_unpack(codes, scales, out=None):
+    """The bf16 values of an 8-bit checkpoint (see dcp_act8_unpack)."""
+    import torch
+    _check_codes(torch, codes, scales)
+    fmt = _act_format(torch, codes)
+    if fmt == ACT_BF16:
+        raise ValueError("codes must be int8 or float8_e4m3fn")
+    _same_device(codes, "codes", [("scales", scales)] + ([("out", out)] if out is not None else []))
+    out = torch.empty(codes.shape, dtype=torch.bfloat16, device=codes.device) if out is None else out
+    ld = _check_rows(torch, out, "out", codes.shape)
+    d = Act8DescC(int(codes.shape[0]), int(codes.shape[1]), fmt, ld)
+    _enqueue(torch, codes.device, load().dcp_act8_unpack, d, codes.data_ptr(), scales.data_ptr(), out.data_ptr())
+    return out
+
+
+def act8_gelu_bwd(codes, scales, da, du=None, a=None):
+    """du = da GELU'(u) and a = GELU(u) from the checkpoint of u (see
+    dcp_act8_gelu_bwd), or from a contiguous bf16 u passed as ``codes`` with
+    ``scales`` None."""
+    import torch
+    if scales is None:
+        if not hasattr(codes, "dim") or codes.dtype != torch.bfloat16 or codes.dim() != 2 or not codes.is_contiguous():
+            raise ValueError("without scales u must be a contiguous bf16 tensor of shape [rows, cols]")
+    else:
+        _check_codes(torch, codes, scales)
+    fmt = _act_format(torch, codes)
+    if (fmt == ACT_BF16) != (scales is None):
+        raise ValueError("scales go with int8 or float8_e4m3fn codes")
+    given = [(n, t) for n, t in (("scales", scales), ("da", da), ("du", du), ("a", a)) if t is not None]
+    for n, t in given[1 if scales is not None else 0:]:
+        _check_rows(torch, t, n, codes.shape)
+        if not t.is_contiguous():
+            raise ValueError(f"{n} must be contiguous")
+    _same_device(codes, "codes", given)
+    du = torch.empty_like(da) if du is None else du
+    a = torch.empty_like(da) if a is None else a
+    rows, cols = (int(n) for n in codes.shape)
+    d = Act8DescC(rows, cols, fmt, cols)
+    _enqueue(torch, da.device, load().dcp_act8_gelu_bwd, d, codes.data_ptr(), None if scales is None else
+             scales.data_ptr(), da.data_ptr(), du.data_ptr(), a.data_ptr())
+    return du, a
+
+
+# ---------------------------------------------------------------------------
+# the gated, normed join of a branch into the residual stream
+
+class GatedNorm(NamedTuple):
+    """What gated_norm_fwd returns; y, the row scales and the checkpoints
+    (codes, scales) of f and out are None where they were not asked for."""
+    out: object
+    y: object
+    rstd_f: object
+    rstd_out: object
+    f8: Optional[Tuple]
+    out8: Optional[Tuple]
+
+
+class GatedNormGrads(NamedTuple):
+    """What gated_norm_bwd returns: bf16 dx, df and (asked for) y; fp32 gradients
+    of the weights that are present."""
+    dx: object
+    df: object
+    y: object
+    dpost: object
+    dgate: object
+    dpre: object
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _join_weights(torch, shape, post, gate, pre, cu_seqlens, device):
+    """Checks the weights of a join over [rows, hidden]; returns (n_seqs, the
+    device tensor of offsets or None)."""
+    rows, h = shape
+    for name, t in (("post", post), ("pre", pre)):
+        if t is not None and (tuple(t.shape) != (h,) or t.dtype != torch.bfloat16 or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous bf16 tensor of shape ({h},)")
+    n = 0
+    if cu_seqlens is not None:
+        if gate is None:
+            raise ValueError("cu_seqlens is for a gate of each sequence, and there is no gate")
+        if not getattr(cu_seqlens, "is_cuda", False):
+            cu = _host_cu(cu_seqlens)
+            if cu[0] != 0 or np.any(np.diff(cu) < 0) or int(cu[-1]) > rows:
+                raise ValueError("cu_seqlens must start at 0, not decrease and end within the rows")
+            cu_seqlens = torch.from_numpy(cu).to(device)
+        elif cu_seqlens.dim() != 1 or cu_seqlens.dtype != torch.int32 or not cu_seqlens.is_contiguous() \
+                or cu_seqlens.numel() < 2:
+            raise ValueError("cu_seqlens on a device must be a contiguous int32 tensor of at least two offsets")
+        n = int(cu_seqlens.numel()) - 1
+    if gate is not None:
+        want = [(n, h)] if n else [(h,), (1, h)]
+        if tuple(gate.shape) not in want or gate.dtype != torch.bfloat16 or not gate.is_contiguous():
+            raise ValueError(f"gate must be a contiguous bf16 tensor of shape {want[0]}")
+    _check_on = [(a, t) for a, t in (("post", post), ("gate", gate), ("pre", pre), ("cu_seqlens", cu_seqlens))
+                 if t is not None]
+    for a, t in _check_on:
+        if t.device != device:
+            raise ValueError(f"{a} is on {t.device}, the activations on {device}")
+    return n, cu_seqlens
+
+
+def _check_matrix(torch, name, t, shape, dtypes=None):
+    if not hasattr(t, "dim") or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be a tensor of shape {tuple(shape)}")
+    if t.dtype not in (dtypes or (torch.bfloat16,)) or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous and bf16" + (" or float32" if dtypes else ""))
+
+
+def gated_norm_fwd(x, f, post=None, gate=None, pre=None, cu_seqlens=None, residual_scale: float = 1.0,
+                   eps: float = 1e-6, keep_f: Optional[str] = None, keep_out: Optional[str] = None, out=None,
+                   y=None) -> GatedNorm:
+    """out = residual_scale x + gate o RMSNorm(f; post), y = RMSNorm(out; pre)
+    (see dcp_gated_norm_fwd).  ``gate``: [hidden] for all rows, or [n_seqs, hidden]
+    with ``cu_seqlens`` (an int32 tensor on the device, used as it is; or host
+    offsets, checked and uploaded); rows behind the last sequence of ``out`` and
+    ``y`` are left as they are.  ``keep_f`` / ``keep_out`` ("int8" or "e4m3", one
+    format a call) also return the checkpoint of f / of out."""
+    import torch
+    if not hasattr(x, "dim") or x.dim() != 2:
+        raise ValueError("x must be a tensor of shape [rows, hidden]")
+    given = [("x", x), ("f", f)] + [(n, t) for n, t in (("out", out), ("y", y)) if t is not None]
+    for n, t in given:
+        _check_matrix(torch, n, t, x.shape)
+    if y is not None and pre is None:
+        raise ValueError("y needs the gain pre")
+    kinds = {k for k in (keep_f, keep_out) if k is not None}
+    if len(kinds) > 1:
+        raise ValueError("keep_f and keep_out must be one format")
+    fmt = kinds.pop() if kinds else "bf16"
+    dtype = None if fmt == "bf16" and keep_f is None and keep_out is None else _act_dtype(torch, fmt)
+    _same_device(x, "x", given[1:])
+    n, cu = _join_weights(torch, x.shape, post, gate, pre, cu_seqlens, x.device)
+    rows, h = (int(v) for v in x.shape)
+    out = torch.empty_like(x) if out is None else out
+    if pre is not None and y is None:
+        y = torch.empty_like(x)
+    row_scale = lambda on: torch.empty(rows, dtype=torch.float32, device=x.device) if on else None
+    rstd_f, rstd_out = row_scale(post is not None), row_scale(pre is not None)
+
+    def kept(on):
+        if on is None:
+            return None, None
+        t = (torch.empty((rows, h), dtype=dtype, device=x.device),
+             torch.empty((rows, -(-h // ACT_GROUP)), dtype=torch.uint8, device=x.device))
+        return t, KeptC(t[0].data_ptr(), t[1].data_ptr())
+
+    (f8, kf), (out8, ko) = kept(keep_f), kept(keep_out)
+    d = GatedNormDescC(rows, h, n, _ptr(cu), float(residual_scale), float(eps), ACT_FORMATS[fmt], 0, 0)
+    w = GatedNormPtrsC(_ptr(post), _ptr(gate), _ptr(pre))
+    _enqueue(torch, x.device, load().dcp_gated_norm_fwd, d, w, x.data_ptr(), f.data_ptr(), out.data_ptr(), _ptr(y),
+             _ptr(rstd_f), _ptr(rstd_out), kf, ko)
+    return GatedNorm(out, y, rstd_f, rstd_out, f8, out8)
+
+
+def gated_norm_bwd(dout, dy=None, f=None, out=None, rstd_f=None, rstd_out=None, post=None, gate=None, pre=None,
+                   cu_seqlens=None, residual_scale: float = 1.0, want_y: bool = False, want_dx: bool = True, dx=None,
+                   df=None, y=None, workspace=None) -> GatedNormGrads:
+    """Backward of gated_norm_fwd (see dcp_gated_norm_bwd).  ``f`` and ``out``: the
+    activations in bf16, or their checkpoints (codes, scales), in one format;
+    ``dy`` bf16 or float32; ``dout`` may be None (zero) where ``pre`` is given;
+    ``want_y`` returns y again, formed from ``out`` as kept.  Rows behind the last
+    sequence are left as they are."""
+    import torch
+    ref = dout if dout is not None else dy
+    if not hasattr(ref, "dim") or ref.dim() != 2:
+        raise ValueError("dout (or, without it, dy) must be a tensor of shape [rows, hidden]")
+    if pre is None and (dy is not None or want_y or y is not None):
+        raise ValueError("dy and y need the gain pre")
+    if pre is not None and dy is None:
+        raise ValueError("the gain pre needs dy")
+    shape = tuple(int(v) for v in ref.shape)
+    rows, h = shape
+    on = []
+    for n_, t in (("dout", dout), ("dx", dx), ("df", df), ("y", y)):
+        if t is not None:
+            _check_matrix(torch, n_, t, shape)
+            on.append((n_, t))
+    if dy is not None:
+        _check_matrix(torch, "dy", dy, shape, (torch.bfloat16, torch.float32))
+        on.append(("dy", dy))
+    fmts = set()
+
+    def kept(name, t, needed):
+        if not needed:
+            return None
+        if t is None:
+            raise ValueError(f"{name} is needed for these weights")
+        if isinstance(t, (tuple, list)):
+            codes, scales = t
+            _check_codes(torch, codes, scales, shape)
+            fmt = _act_format(torch, codes)
+            if fmt == ACT_BF16:
+                raise ValueError(f"{name}: codes must be int8 or float8_e4m3fn")
+            fmts.add(fmt)
+            on.extend([(name, codes), (name + "'s scales", scales)])
+            return KeptC(codes.data_ptr(), scales.data_ptr())
+        _check_matrix(torch, name, t, shape)
+        fmts.add(ACT_BF16)
+        on.append((name, t))
+        return KeptC(t.data_ptr(), None)
+
+    kf = kept("f", f, post is not None or gate is not None)
+    ko = kept("out", out, pre is not None)
+    if len(fmts) > 1:
+        raise ValueError("f and out must be kept in one format")
+    for n_, t, needed in (("rstd_f", rstd_f, post is not None), ("rstd_out", rstd_out, pre is not None)):
+        if needed:
+            if not hasattr(t, "dim") or tuple(t.shape) != (rows,) or t.dtype != torch.float32 or not t.is_contiguous():
+                raise ValueError(f"{n_} must be a contiguous float32 tensor of shape ({rows},)")
+            on.append((n_, t))
+    if workspace is not None:
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+        on.append(("workspace", workspace))
+    _same_device(ref, "dout", on)
+    n, cu = _join_weights(torch, shape, post, gate, pre, cu_seqlens, ref.device)
+    lib = load()
+    d = GatedNormDescC(rows, h, n, _ptr(cu), float(residual_scale), 0.0, fmts.pop() if fmts else ACT_BF16,
+                       int(dy is not None and dy.dtype == torch.float32), 0)
+    w = GatedNormPtrsC(_ptr(post), _ptr(gate), _ptr(pre))
+    size = C.c_size_t()
+    _check(lib.dcp_gated_norm_bwd_workspace_size(d, C.byref(size)))
+    empty = lambda: torch.empty(shape, dtype=torch.bfloat16, device=ref.device)
+    if want_dx and dx is None:
+        dx = empty()
+    df = empty() if df is None else df
+    if want_y and y is None:
+        y = empty()
+    grad = lambda t: None if t is None else torch.empty(t.shape, dtype=torch.float32, device=ref.device)
+    dpost, dgate, dpre = grad(post), grad(gate), grad(pre)
+    if workspace is None:
+        workspace = torch.empty(size.value, dtype=torch.uint8, device=ref.device)
+    _enqueue(torch, ref.device, lib.dcp_gated_norm_bwd, d, w, _ptr(dout), _ptr(dy), kf, ko, _ptr(rstd_f),
+             _ptr(rstd_out), _ptr(dx), df.data_ptr(), _ptr(y), GatedNormPtrsC(_ptr(dpost), _ptr(dgate), _ptr(dpre)),
+             workspace.data_ptr(), _nbytes(workspace))
+    return GatedNormGrads(dx, df, y, dpost, dgate, dpre)
