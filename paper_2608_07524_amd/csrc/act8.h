@@ -38,17 +38,24 @@ __device__ __forceinline__ float dpp_add(float v) {
 }
 constexpr int kQuadXor1 = 0xB1, kQuadXor2 = 0x4E, kHalfMirror = 0x141, kMirror = 0x140;
 
-// Sum over the wavefront, the same in every lane: within 16 lanes by data-parallel
-// moves of the vector ALU, across them by lane swaps; no trip through LDS.
-__device__ __forceinline__ float wave_total(float v) {
-  v = dpp_add<kQuadXor1>(v);
-  v = dpp_add<kQuadXor2>(v);
-  v = dpp_add<kHalfMirror>(v);
-  v = dpp_add<kMirror>(v);
-  u32x2 s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
-  s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+// Sum over each aligned run of L lanes (a power of two up to 64), the same in all
+// of them: within 16 lanes by data-parallel moves of the vector ALU, across them by
+// lane swaps; no trip through LDS.
+template <int L>
+__device__ __forceinline__ float lane_total(float v) {
+  if constexpr (L >= 2) v = dpp_add<kQuadXor1>(v);
+  if constexpr (L >= 4) v = dpp_add<kQuadXor2>(v);
+  if constexpr (L >= 8) v = dpp_add<kHalfMirror>(v);
+  if constexpr (L >= 16) v = dpp_add<kMirror>(v);
+  if constexpr (L >= 32) {
+    const u32x2 s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+  }
+  if constexpr (L >= 64) {
+    const u32x2 s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+  }
+  return v;
 }
 
 // Largest magnitude of a lane's 8 values, as bf16 bits (ordered as integers, NaN
@@ -125,6 +132,25 @@ __device__ __forceinline__ void decode8(u32x2 c, uint32_t b, float (&x)[8]) {
   }
 }
 
+// The same times m, rounded once (|code 2^k m| far below 2^121: the int8 form passes
+// 128 2^k m).
+template <int FMT>
+__device__ __forceinline__ void decode8_scaled(u32x2 c, uint32_t b, float m, float (&x)[8]) {
+  if constexpr (FMT == DCP_ACT_INT8) {
+    const float s = __uint_as_float(b << 23) * m, off = -128.f * s;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t u = c[h] ^ 0x80808080u;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[4 * h + i] = __builtin_fmaf(float((u >> (8 * i)) & 0xffu), s, off);
+    }
+  } else {
+    decode8<FMT>(c, b, x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] *= m;
+  }
+}
+
 // Eight consecutive values of a stored activation: bf16, or codes and their byte.
 template <int FMT>
 struct Held8 {
@@ -135,6 +161,7 @@ struct Held8 {
     b = scales[group];
   }
   __device__ __forceinline__ void get(float (&x)[8]) const { decode8<FMT>(c, b, x); }
+  __device__ __forceinline__ void get_scaled(float m, float (&x)[8]) const { decode8_scaled<FMT>(c, b, m, x); }
 };
 template <>
 struct Held8<DCP_ACT_BF16> {
@@ -145,6 +172,10 @@ struct Held8<DCP_ACT_BF16> {
   __device__ __forceinline__ void get(float (&x)[8]) const {
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = float(v[i]);
+  }
+  __device__ __forceinline__ void get_scaled(float m, float (&x)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = float(v[i]) * m;
   }
 };
 

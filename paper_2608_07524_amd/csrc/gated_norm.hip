@@ -12,69 +12,116 @@
 //   dpre = sum_t dy o oh.
 // HBM-bound: every input is read once and every output written once, all of a row
 // in registers between; sums, statistics and gradients of the parameters are fp32.
+#include <type_traits>
+
 #include "act8.h"
 #include "block_launch.h"
 
 namespace dcp {
 namespace {
 
-// A team of W wavefronts owns a row: lane l of the team has columns 8 l + 512 W c,
-// c < NC (the last chunk may be partly idle), so one access is 16 bytes a lane.
-// Teams take kFwdRows consecutive rows (so that gains, gate and the place in
-// cu_seqlens are fetched once); a workgroup is 4 wavefronts.
-constexpr int kFwdRows = 8;
+// A team of TL lanes owns a row, 8 columns (one 16-byte access) a lane: the power
+// of two up to 64, or the multiple of 64, that covers hidden / 8.  One piece a lane
+// keeps the backward at a hundred registers, so that four wavefronts share a SIMD and
+// loads are always in flight; with three pieces (one wavefront for hidden 1,152) it
+// took 259, one wavefront a SIMD, and twice the time.  Teams take consecutive rows:
+// gains, gate and the place in cu_seqlens are fetched once, and the next row is
+// loaded before the present one is worked on.  A workgroup is one team of more than
+// 128 lanes or 256 lanes of smaller ones.
+template <int TL>
+struct Team {
+  static constexpr int kBlock = TL > 128 ? TL : 256, kTeams = kBlock / TL;
+  static constexpr int kSub = TL < 64 ? TL : 64;       // lanes of a team within a wavefront
+  static constexpr int kWaves = TL < 64 ? 1 : TL / 64;  // wavefronts a team spans
+};
 
-template <int W>
-__device__ __forceinline__ float team_total(float v, float* red) {
-  v = wave_total(v);
-  if constexpr (W > 1) {
-    const int wave = threadIdx.x >> 6;
-    __syncthreads();  // (the last sum's readers are done)
-    red[wave] = v;
-    __syncthreads();
-    const int first = wave / W * W;
-    v = red[first];
+// Sums of N values over a team.  Teams of several wavefronts meet once, in the half
+// of `red` that belongs to this row's parity: the other half's readers are at most
+// one barrier behind.
+template <int TL, int N>
+__device__ __forceinline__ void team_total(float (&v)[N], float* red, int parity) {
 #pragma unroll
-    for (int w = 1; w < W; ++w) v += red[first + w];
+  for (int n = 0; n < N; ++n) v[n] = lane_total<Team<TL>::kSub>(v[n]);
+  if constexpr (Team<TL>::kWaves > 1) {
+    constexpr int kWaves = Team<TL>::kBlock / 64;
+    const int wave = threadIdx.x >> 6, first = wave / Team<TL>::kWaves * Team<TL>::kWaves;
+    float* r = red + parity * kWaves * N;
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+      for (int n = 0; n < N; ++n) r[wave * N + n] = v[n];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      float t = r[first * N + n];
+#pragma unroll
+      for (int w = 1; w < Team<TL>::kWaves; ++w) t += r[(first + w) * N + n];
+      v[n] = t;
+    }
   }
-  return v;
 }
 
 // The sequence of `row`: the last index s <= n with cu[s] <= row (n: the row lies
-// behind the last sequence).  64 probes a step, so three steps reach 2^18
-// sequences.  Whatever cu holds, s stays in [0, n].
+// behind the last sequence), by as many probes a step as the team has lanes in the
+// wavefront (64: three steps reach 2^18 sequences).  Whatever cu holds, s stays in
+// [0, n].
+template <int L>
 __device__ __forceinline__ int sequence_of(const int32_t* cu, int n, int64_t row) {
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & (L - 1), shift = threadIdx.x & 63 & ~(L - 1);
+  const uint64_t mask = L == 64 ? ~uint64_t(0) : (uint64_t(1) << (L & 63)) - 1;
   int lo = 0, len = n + 1;
   while (len > 1) {
-    const int step = (len + 63) >> 6, at = lane * step;
+    const int step = (len + L - 1) / L, at = lane * step;
     const bool below = at < len && int64_t(cu[lo + at]) <= row;
-    const int c = max(int(__popcll(__ballot(below))) - 1, 0);
+    const int c = max(int(__popcll((__ballot(below) >> shift) & mask)) - 1, 0);
     lo += c * step;
     len = min(step, len - c * step);
-    if (len < 1) len = 1;  // (only if cu is not sorted)
   }
-  return min(lo, n);
+  return lo;
 }
 
-// Follows consecutive rows through cu_seqlens.
+// Follows a team's consecutive rows through cu_seqlens.
 struct Walk {
   const int32_t* cu;
   int n, s;
   int64_t end;  // first row behind sequence s
+  template <int L>
   __device__ __forceinline__ void start(const int32_t* c, int n_seqs, int64_t row) {
     cu = c;
     n = n_seqs;
-    s = __builtin_amdgcn_readfirstlane(min(sequence_of(c, n_seqs, row), n_seqs - 1));
+    s = min(sequence_of<L>(c, n_seqs, row), n_seqs - 1);
     end = cu[s + 1];
   }
-  // whether `row` lies in a later sequence than the row before
-  __device__ __forceinline__ bool step(int64_t row) {
-    if (row < end) return false;
+  // to the sequence of `row`, if that is a later one
+  __device__ __forceinline__ void step(int64_t row) {
     while (row >= end && s < n - 1) end = cu[++s + 1];
-    return true;
   }
 };
+
+// 8 values of a bf16 row at column c as fp32, 1 where there is none.
+__device__ __forceinline__ void gains(const __bf16* g, int c, int h, float (&v)[8]) {
+  if (g && c < h) {
+    const bf16x8 b = *reinterpret_cast<const bf16x8*>(g + c);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = float(b[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = 1.f;
+  }
+}
+__device__ __forceinline__ void gains_product(const __bf16* a, const __bf16* b, int c, int h, float (&v)[8]) {
+  float w[8];
+  gains(a, c, h, v);
+  gains(b, c, h, w);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] *= w[e];
+}
+__device__ __forceinline__ bf16x8 rounded(const float (&v)[8]) {
+  bf16x8 b;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) b[e] = __bf16(v[e]);
+  return b;
+}
 
 template <int FMT>
 __device__ __forceinline__ void keep8(void* codes, void* scales, bf16x8 v, int64_t row, int c, int h, int groups) {
@@ -83,120 +130,116 @@ __device__ __forceinline__ void keep8(void* codes, void* scales, bf16x8 v, int64
   if (c < h && (c & 31) == 0) static_cast<uint8_t*>(scales)[row * groups + (c >> 5)] = uint8_t(byte);
 }
 
-// KEEP: format of the checkpoints (DCP_ACT_BF16: none).  y, its statistics and the
-// checkpoint of out come from out in fp32 and from out as stored, respectively.
-template <int W, int NC, int KEEP>
-__global__ __launch_bounds__(256) void gated_norm_fwd_kernel(GatedNormFwd p) {
-  __shared__ float red[4];
-  const int lane = threadIdx.x % (64 * W), team = threadIdx.x / (64 * W);
-  const int h = p.hidden, groups = (h + kActGroup - 1) / kActGroup;
-  const int64_t first = (int64_t(blockIdx.x) * (4 / W) + team) * kFwdRows;
+// KEEP: format of the checkpoints (DCP_ACT_BF16: none).  y and its statistics come
+// from out in fp32, the checkpoint of out from out as stored.
+template <int TL, int KEEP>
+__global__ __launch_bounds__(Team<TL>::kBlock) void gated_norm_fwd_kernel(GatedNormFwd p, int team_rows) {
+  using T = Team<TL>;
+  __shared__ float red[2][2][T::kBlock / 64];
+  const int lane = threadIdx.x % TL, c = 8 * lane, h = p.hidden, groups = (h + kActGroup - 1) / kActGroup;
+  const bool mine = c < h;
+  const int64_t block_first = int64_t(blockIdx.x) * T::kTeams * team_rows;
+  const int64_t first = block_first + int64_t(threadIdx.x / TL) * team_rows;
   int64_t rows = p.rows;
   if (p.cu) rows = min(rows, int64_t(p.cu[p.n_seqs]));
-  if (W == 1 && first >= rows) return;
+  if (block_first >= rows) return;
+  // (teams that meet at barriers all take the first team's turns)
+  const int64_t left = rows - (T::kWaves > 1 ? block_first : first);
+  const int turns = int(min(left, int64_t(team_rows)));
   const __bf16 *x = static_cast<const __bf16*>(p.x), *f = static_cast<const __bf16*>(p.f);
-  const __bf16 *gate = static_cast<const __bf16*>(p.gate);
-  bf16x8 post[NC], pre[NC], gt[NC];
-  auto row_of = [&](const __bf16* g, bf16x8 (&v)[NC]) {
-#pragma unroll
-    for (int k = 0; k < NC; ++k) {
-      const int c = 8 * lane + 512 * W * k;
-      if (c < h && g) {
-        v[k] = *reinterpret_cast<const bf16x8*>(g + c);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[k][e] = __bf16(1.f);
-      }
+  const __bf16 *post = static_cast<const __bf16*>(p.post), *gate = static_cast<const __bf16*>(p.gate);
+  bf16x8 xn{}, fn{};
+  auto fetch = [&](int64_t row) {
+    if (mine && row < rows) {
+      fn = *reinterpret_cast<const bf16x8*>(f + row * h + c);
+      xn = *reinterpret_cast<const bf16x8*>(x + row * h + c);
     }
   };
-  row_of(static_cast<const __bf16*>(p.post), post);
-  row_of(static_cast<const __bf16*>(p.pre), pre);
+  fetch(first);
+  float branch[8], pre[8];  // post o gate, pre
+  gains(static_cast<const __bf16*>(p.pre), c, h, pre);
   Walk walk;
-  if (p.cu && first < rows) {
-    walk.start(p.cu, p.n_seqs, first);
-    row_of(gate + int64_t(walk.s) * h, gt);
-  } else {
-    row_of(gate, gt);
-  }
-  for (int i = 0; i < kFwdRows; ++i) {
+  walk.s = 0;
+  walk.end = INT64_MAX;
+  if (p.cu && first < rows) walk.start<T::kSub>(p.cu, p.n_seqs, first);
+  gains_product(post, gate ? gate + int64_t(walk.s) * h : nullptr, c, h, branch);
+  for (int i = 0; i < turns; ++i) {
     const int64_t row = first + i;
     const bool live = row < rows;
-    if (W == 1 && !live) break;
-    if (p.cu && i > 0 && live && walk.step(row)) row_of(gate + int64_t(walk.s) * h, gt);
-    bf16x8 xv[NC], fv[NC];
-#pragma unroll
-    for (int k = 0; k < NC; ++k) {
-      const int c = 8 * lane + 512 * W * k;
-      xv[k] = fv[k] = bf16x8{};
-      if (live && c < h) {
-        fv[k] = *reinterpret_cast<const bf16x8*>(f + row * h + c);
-        xv[k] = *reinterpret_cast<const bf16x8*>(x + row * h + c);
-      }
+    if (live && row >= walk.end) {
+      walk.step(row);
+      gains_product(post, gate + int64_t(walk.s) * h, c, h, branch);
     }
-    float rf = 1.f;
+    const bf16x8 xv = xn, fv = fn;
+    if (i + 1 < turns) fetch(row + 1);
+    float fx[8], r[1] = {0.f}, rf = 1.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      fx[e] = float(fv[e]);
+      r[0] += fx[e] * fx[e];
+    }
     if (p.post) {
-      float ss = 0.f;
-#pragma unroll
-      for (int k = 0; k < NC; ++k)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) ss += float(fv[k][e]) * float(fv[k][e]);
-      rf = rsqrtf(team_total<W>(ss, red) / float(h) + p.eps);
+      team_total<TL>(r, red[0][0], i & 1);
+      rf = rsqrtf(r[0] / float(h) + p.eps);
       if (live && lane == 0) p.rstd_f[row] = rf;
     }
-    float o[NC][8], ss = 0.f;
+    float o[8];
+    r[0] = 0.f;
 #pragma unroll
-    for (int k = 0; k < NC; ++k) {
-      const int c = 8 * lane + 512 * W * k;
-      bf16x8 ov;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        o[k][e] = p.alpha * float(xv[k][e]) + float(gt[k][e]) * (float(fv[k][e]) * rf * float(post[k][e]));
-        ss += o[k][e] * o[k][e];
-        ov[e] = __bf16(o[k][e]);
-      }
-      if (live && c < h) *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.out) + row * h + c) = ov;
-      if constexpr (KEEP != DCP_ACT_BF16) {
-        if (live && p.keep_f) keep8<KEEP>(p.keep_f, p.keep_f_scales, fv[k], row, c, h, groups);
-        if (live && p.keep_out) keep8<KEEP>(p.keep_out, p.keep_out_scales, ov, row, c, h, groups);
-      }
+    for (int e = 0; e < 8; ++e) {
+      o[e] = p.alpha * float(xv[e]) + branch[e] * (fx[e] * rf);
+      r[0] += o[e] * o[e];
+    }
+    const bf16x8 ov = rounded(o);
+    if (live && mine) *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.out) + row * h + c) = ov;
+    if constexpr (KEEP != DCP_ACT_BF16) {
+      if (live && p.keep_f) keep8<KEEP>(p.keep_f, p.keep_f_scales, fv, row, c, h, groups);
+      if (live && p.keep_out) keep8<KEEP>(p.keep_out, p.keep_out_scales, ov, row, c, h, groups);
     }
     if (p.pre) {
-      const float ro = rsqrtf(team_total<W>(ss, red) / float(h) + p.eps);
+      team_total<TL>(r, red[1][0], i & 1);
+      const float ro = rsqrtf(r[0] / float(h) + p.eps);
       if (live && lane == 0) p.rstd_out[row] = ro;
 #pragma unroll
-      for (int k = 0; k < NC; ++k) {
-        const int c = 8 * lane + 512 * W * k;
-        bf16x8 yv;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) yv[e] = __bf16(o[k][e] * ro * float(pre[k][e]));
-        if (live && c < h) *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.y) + row * h + c) = yv;
-      }
+      for (int e = 0; e < 8; ++e) o[e] *= ro * pre[e];
+      if (live && mine) *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.y) + row * h + c) = rounded(o);
     }
   }
 }
 
-// Backward.  Teams take `team_rows` consecutive rows and keep the column sums of
-// G o fh and dy o oh in registers: one partial row a workgroup for dpost (or A with
-// one gate row) and dpre, and, with a gate for each sequence, A_s either straight
-// into dgate (a sequence whose rows all lie in one team) or as a partial row of the
-// team: slot 0 for the sequence that its first row belongs to, slot 1 for one that
-// starts inside and goes on.  A second launch adds the partial rows in a fixed
-// order, so results are bitwise reproducible.
-constexpr int kBwdRowsMin = 4, kBwdRowsMax = 64, kBwdTeams = 4096;
-
+// Backward.  A lane keeps its columns' sums of G o fh and dy o oh over the team's
+// rows: one partial row a workgroup for dpost (or A with one gate row) and dpre, and,
+// with a gate for each sequence, A_s either straight into dgate (a sequence whose
+// rows all lie in one team) or as a partial row of the team: slot 0 for the sequence
+// that its first row belongs to, slot 1 for one that starts inside and goes on.  A
+// second launch adds the partial rows in a fixed order, so results are bitwise
+// reproducible.
+//
+// The two means of a row need one meeting of the team: with t = dout + r_o d and m =
+// mean(d oh), G = t - r_o m oh, so mean(e fh) = mean(b t) - r_o m mean(b oh), b = post
+// o gate o fh.
 struct BwdShape {
-  int team_rows, waves;  // rows of a team, wavefronts of a team
-  int64_t teams, blocks;
+  int lanes, block, teams_of_block, team_rows;
+  int64_t blocks, teams;
 };
-inline int team_waves(int hidden) { return hidden <= 1536 ? 1 : hidden <= 3072 ? 2 : 4; }
+inline int team_lanes(int hidden) {
+  const int need = (hidden + 7) / 8;
+  if (need > 64) return (need + 63) / 64 * 64;
+  int l = 8;
+  while (l < need) l *= 2;
+  return l;
+}
 inline BwdShape bwd_shape(int64_t rows, int hidden) {
   BwdShape s;
-  s.waves = team_waves(hidden);
-  const int64_t want = (rows + kBwdTeams / s.waves - 1) / (kBwdTeams / s.waves);
-  s.team_rows = int(want < kBwdRowsMin ? kBwdRowsMin : want > kBwdRowsMax ? kBwdRowsMax : want);
-  s.teams = (rows + s.team_rows - 1) / s.team_rows;
-  s.blocks = (s.teams + 4 / s.waves - 1) / (4 / s.waves);
-  s.teams = s.blocks * (4 / s.waves);
+  s.lanes = team_lanes(hidden);
+  s.block = s.lanes > 128 ? s.lanes : 256;
+  s.teams_of_block = s.block / s.lanes;
+  // rows of a team: few rows, short chains; many, few partial rows
+  s.team_rows = 1;
+  while (s.team_rows < 64 && int64_t(64) * s.team_rows * s.team_rows < rows) ++s.team_rows;
+  const int64_t per_block = int64_t(s.teams_of_block) * s.team_rows;
+  s.blocks = (rows + per_block - 1) / per_block;
+  s.teams = s.blocks * s.teams_of_block;
   return s;
 }
 
@@ -206,221 +249,159 @@ struct BwdParts {
   int team_rows;
 };
 
-template <int W, int NC, int FMT, bool DY32>
-__global__ __launch_bounds__(256) void gated_norm_bwd_kernel(GatedNormBwd p, BwdParts w) {
-  __shared__ float red[4];
-  extern __shared__ float sums[];  // [4 / W teams][h]
-  constexpr int kTeams = 4 / W;
-  const int lane = threadIdx.x % (64 * W), team = threadIdx.x / (64 * W);
+template <int TL, int FMT, bool DY32>
+__global__ __launch_bounds__(Team<TL>::kBlock) void gated_norm_bwd_kernel(GatedNormBwd p, BwdParts w) {
+  using T = Team<TL>;
+  __shared__ float red[2][3 * (T::kBlock / 64)];
+  __shared__ float sums[T::kTeams][8 * TL];
+  const int team = threadIdx.x / TL, lane = threadIdx.x % TL, c = 8 * lane;
   const int h = p.hidden, groups = (h + kActGroup - 1) / kActGroup;
-  const int64_t first = (int64_t(blockIdx.x) * kTeams + team) * w.team_rows;
+  const bool mine = c < h;
+  const int64_t block_first = int64_t(blockIdx.x) * T::kTeams * w.team_rows;
+  const int64_t first = block_first + int64_t(team) * w.team_rows;
   int64_t rows = p.rows;
   if (p.cu) rows = min(rows, int64_t(p.cu[p.n_seqs]));
+  const int64_t left = rows - (T::kWaves > 1 ? block_first : first);
+  const int turns = int(max(min(left, int64_t(w.team_rows)), int64_t(0)));
   const bool has_f = p.post != nullptr || p.gate != nullptr;
-  const __bf16 *dout = static_cast<const __bf16*>(p.dout), *gate = static_cast<const __bf16*>(p.gate);
-  bf16x8 post[NC], pre[NC], gt[NC];
-  float acc_pre[NC][8], acc_a[NC][8];
-  auto row_of = [&](const __bf16* g, bf16x8 (&v)[NC]) {
-#pragma unroll
-    for (int k = 0; k < NC; ++k) {
-      const int c = 8 * lane + 512 * W * k;
-      if (c < h && g) {
-        v[k] = *reinterpret_cast<const bf16x8*>(g + c);
+  const __bf16 *dout = static_cast<const __bf16*>(p.dout);
+  const __bf16 *post = static_cast<const __bf16*>(p.post), *gate = static_cast<const __bf16*>(p.gate);
+
+  bf16x8 gn{}, dn{};
+  f32x4 dn32[2] = {};
+  Held8<FMT> fn{}, on{};
+  float rfn = 1.f, ron = 0.f;
+  auto fetch = [&](int64_t row) {
+    if (row >= rows) return;
+    if (p.post) rfn = p.rstd_f[row];
+    if (p.pre) ron = p.rstd_out[row];
+    if (!mine) return;
+    const int64_t at = row * h + c, grp = row * groups + (c >> 5);
+    if (dout) gn = *reinterpret_cast<const bf16x8*>(dout + at);
+    if (p.pre) {
+      on.load(p.out, static_cast<const uint8_t*>(p.out_scales), at, grp);
+      if constexpr (DY32) {
+        dn32[0] = *reinterpret_cast<const f32x4*>(static_cast<const float*>(p.dy) + at);
+        dn32[1] = *reinterpret_cast<const f32x4*>(static_cast<const float*>(p.dy) + at + 4);
       } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[k][e] = __bf16(1.f);
+        dn = *reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(p.dy) + at);
       }
     }
+    if (has_f) fn.load(p.f, static_cast<const uint8_t*>(p.f_scales), at, grp);
   };
-  row_of(static_cast<const __bf16*>(p.post), post);
-  row_of(static_cast<const __bf16*>(p.pre), pre);
-#pragma unroll
-  for (int k = 0; k < NC; ++k)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) acc_pre[k][e] = acc_a[k][e] = 0.f;
-  float* mine = sums + team * h;
+  fetch(first);
+  float branch[8], pre[8], acc_pre[8], acc_a[8];  // post o gate, pre; sums of dy o oh, G o fh
+  gains(static_cast<const __bf16*>(p.pre), c, h, pre);
   Walk walk;
   walk.s = 0;
-  walk.end = 0;
-  int64_t from = first;  // first row of the team's current sequence
-  if (p.cu && first < rows) {
-    walk.start(p.cu, p.n_seqs, first);
-    row_of(gate + int64_t(walk.s) * h, gt);
-  } else {
-    row_of(p.cu ? nullptr : gate, gt);
+  walk.end = INT64_MAX;
+  int64_t from = first;  // first of the team's rows in the current sequence
+  if (p.cu && first < rows) walk.start<T::kSub>(p.cu, p.n_seqs, first);
+  gains_product(post, gate ? gate + int64_t(walk.s) * h : nullptr, c, h, branch);
+  float* sum = &sums[team][c];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    acc_pre[e] = acc_a[e] = 0.f;
+    sum[e] = 0.f;
   }
+  // The team's sum of G o fh over rows [from, to) of the current sequence leaves the
+  // registers.
+  auto flush = [&](int64_t to) {
+    if (!mine) return;
+    const bool starts = int64_t(p.cu[walk.s]) >= first, whole = starts && to >= min(walk.end, rows);
+    float* dst = (whole ? p.dgate + int64_t(walk.s) * h
+                        : w.seg + ((int64_t(blockIdx.x) * T::kTeams + team) * 2 + (from > first ? 1 : 0)) * h) + c;
+    float g[8], q[8];
+    gains(gate + int64_t(walk.s) * h, c, h, g);
+    gains(post, c, h, q);
 #pragma unroll
-  for (int k = 0; k < NC; ++k) {
-    const int c = 8 * lane + 512 * W * k;
-    if (c < h)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) mine[c + e] = 0.f;
-  }
-  // The team's sum of G o fh over rows [from, to) of sequence s leaves the registers.
-  auto flush = [&](int s, int64_t from_, int64_t to, int64_t seq_end) {
-    const bool starts = int64_t(p.cu[s]) >= first, ends = to >= min(seq_end, rows);
-    float* dst = starts && ends ? p.dgate + int64_t(s) * h
-                                : w.seg + ((int64_t(blockIdx.x) * kTeams + team) * 2 + (from_ > first ? 1 : 0)) * h;
-#pragma unroll
-    for (int k = 0; k < NC; ++k) {
-      const int c = 8 * lane + 512 * W * k;
-      if (c < h)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          float v = acc_a[k][e];
-          mine[c + e] += float(gt[k][e]) * v;
-          if (starts && ends) {
-            v *= float(post[k][e]);
-            if (p.accumulate) v += dst[c + e];
-          }
-          dst[c + e] = v;
-          acc_a[k][e] = 0.f;
-        }
+    for (int e = 0; e < 8; ++e) {
+      sum[e] += g[e] * acc_a[e];
+      float v = acc_a[e];
+      if (whole) {
+        v *= q[e];
+        if (p.accumulate) v += dst[e];
+      }
+      dst[e] = v;
+      acc_a[e] = 0.f;
     }
   };
-  for (int i = 0; i < w.team_rows; ++i) {
+  for (int i = 0; i < turns; ++i) {
     const int64_t row = first + i;
     const bool live = row < rows;
-    if (W == 1 && !live) break;
-    if (p.cu && i > 0 && live) {
-      const int s = walk.s;
-      const int64_t e = walk.end;
-      if (walk.step(row)) {
-        flush(s, from, row, e);
-        from = row;
-        row_of(gate + int64_t(walk.s) * h, gt);
-      }
+    if (live && row >= walk.end) {
+      flush(row);
+      from = row;
+      walk.step(row);
+      gains_product(post, gate + int64_t(walk.s) * h, c, h, branch);
     }
-    bf16x8 gv[NC];
-    float d[NC][8];
-    Held8<FMT> fv[NC], ov[NC];
-    float rf = 1.f, ro = 0.f;
-    if (live && p.post) rf = p.rstd_f[row];
-    if (live && p.pre) ro = p.rstd_out[row];
+    float t[8], d[8], oh[8], fh[8];
+    const float rf = rfn, ro = ron;
 #pragma unroll
-    for (int k = 0; k < NC; ++k) {
-      const int c = 8 * lane + 512 * W * k;
-      gv[k] = bf16x8{};
-      fv[k] = ov[k] = Held8<FMT>{};
-#pragma unroll
-      for (int e = 0; e < 8; ++e) d[k][e] = 0.f;
-      if (live && c < h) {
-        const int64_t at = row * h + c, grp = row * groups + (c >> 5);
-        if (dout) gv[k] = *reinterpret_cast<const bf16x8*>(dout + at);
-        if (p.pre) {
-          ov[k].load(p.out, static_cast<const uint8_t*>(p.out_scales), at, grp);
-          if constexpr (DY32) {
-            const f32x4 a = *reinterpret_cast<const f32x4*>(static_cast<const float*>(p.dy) + at);
-            const f32x4 b = *reinterpret_cast<const f32x4*>(static_cast<const float*>(p.dy) + at + 4);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              d[k][e] = a[e];
-              d[k][e + 4] = b[e];
-            }
-          } else {
-            const bf16x8 a = *reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(p.dy) + at);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) d[k][e] = float(a[e]);
-          }
-        }
-        if (has_f) fv[k].load(p.f, static_cast<const uint8_t*>(p.f_scales), at, grp);
-      }
+    for (int e = 0; e < 8; ++e) {
+      t[e] = float(gn[e]);
+      d[e] = DY32 ? dn32[e >> 2][e & 3] : float(dn[e]);
     }
-    float G[NC][8];
+    on.get_scaled(ro, oh);
+    fn.get_scaled(rf, fh);
+    if (!mine || !live) {
 #pragma unroll
-    for (int k = 0; k < NC; ++k)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) G[k][e] = float(gv[k][e]);
-    if (p.pre) {
-      float dot = 0.f;
-      float oh[NC][8];
-#pragma unroll
-      for (int k = 0; k < NC; ++k) {
-        const int c = 8 * lane + 512 * W * k;
-        ov[k].get(oh[k]);
-        bf16x8 yv;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          oh[k][e] = c < h ? oh[k][e] * ro : 0.f;
-          acc_pre[k][e] += d[k][e] * oh[k][e];
-          d[k][e] *= float(pre[k][e]);
-          dot += d[k][e] * oh[k][e];
-          yv[e] = __bf16(oh[k][e] * float(pre[k][e]));
-        }
-        if (live && p.y && c < h) *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.y) + row * h + c) = yv;
-      }
-      const float mean = team_total<W>(dot, red) / float(h);
-#pragma unroll
-      for (int k = 0; k < NC; ++k)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) G[k][e] += ro * (d[k][e] - oh[k][e] * mean);
+      for (int e = 0; e < 8; ++e) t[e] = d[e] = oh[e] = fh[e] = 0.f;
     }
-    if (p.dx) {
+    if (i + 1 < turns) fetch(row + 1);
+    float r[3] = {0.f, 0.f, 0.f};
 #pragma unroll
-      for (int k = 0; k < NC; ++k) {
-        const int c = 8 * lane + 512 * W * k;
-        bf16x8 v;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = __bf16(p.alpha * G[k][e]);
-        if (live && c < h) *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.dx) + row * h + c) = v;
-      }
+    for (int e = 0; e < 8; ++e) {
+      acc_pre[e] += d[e] * oh[e];
+      d[e] *= pre[e];
+      t[e] += ro * d[e];
+      r[0] += d[e] * oh[e];
+      const float b = branch[e] * fh[e];
+      r[1] += b * t[e];
+      r[2] += b * oh[e];
     }
-    float dot = 0.f;
-    float fh[NC][8];
+    if (live && mine && p.y) {
+      float y[8];
 #pragma unroll
-    for (int k = 0; k < NC; ++k) {
-      const int c = 8 * lane + 512 * W * k;
-      fv[k].get(fh[k]);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        fh[k][e] = c < h ? fh[k][e] * rf : 0.f;
-        acc_a[k][e] += G[k][e] * fh[k][e];
-        G[k][e] *= float(gt[k][e]) * float(post[k][e]);
-        dot += G[k][e] * fh[k][e];
-      }
+      for (int e = 0; e < 8; ++e) y[e] = oh[e] * pre[e];
+      *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.y) + row * h + c) = rounded(y);
     }
-    float mean = 0.f;
-    if (p.post) mean = team_total<W>(dot, red) / float(h);
+    team_total<TL>(r, red[0], i & 1);
+    const float m = ro * (r[0] / float(h));
+    const float mf = p.post ? (r[1] - m * r[2]) / float(h) : 0.f;
+    float u[8];
 #pragma unroll
-    for (int k = 0; k < NC; ++k) {
-      const int c = 8 * lane + 512 * W * k;
-      bf16x8 v;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = __bf16(rf * (G[k][e] - fh[k][e] * mean));
-      if (live && p.df && c < h) *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.df) + row * h + c) = v;
+    for (int e = 0; e < 8; ++e) {
+      t[e] -= m * oh[e];  // G
+      acc_a[e] += t[e] * fh[e];
+      u[e] = rf * (branch[e] * t[e] - mf * fh[e]);
+      t[e] *= p.alpha;
+    }
+    if (live && mine) {
+      if (p.dx) *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.dx) + row * h + c) = rounded(t);
+      *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.df) + row * h + c) = rounded(u);
     }
   }
   if (p.cu) {
-    if (first < rows) flush(walk.s, from, min(first + w.team_rows, rows), walk.end);
+    if (first < rows) flush(min(first + w.team_rows, rows));
   } else {
 #pragma unroll
-    for (int k = 0; k < NC; ++k) {
-      const int c = 8 * lane + 512 * W * k;
-      if (c < h)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) mine[c + e] = acc_a[k][e];
-    }
+    for (int e = 0; e < 8; ++e) sum[e] = acc_a[e];
   }
   auto add_teams = [&](float* dst) {
     __syncthreads();
-    for (int c = threadIdx.x; c < h; c += 256) {
-      float t = sums[c];
+    for (int k = threadIdx.x; k < h; k += T::kBlock) {
+      float v = sums[0][k];
 #pragma unroll
-      for (int j = 1; j < kTeams; ++j) t += sums[j * h + c];
-      dst[int64_t(blockIdx.x) * h + c] = t;
+      for (int j = 1; j < T::kTeams; ++j) v += sums[j][k];
+      dst[int64_t(blockIdx.x) * h + k] = v;
     }
     __syncthreads();
   };
   if (has_f) add_teams(w.post);
   if (p.pre) {
-    if (!has_f) __syncthreads();
 #pragma unroll
-    for (int k = 0; k < NC; ++k) {
-      const int c = 8 * lane + 512 * W * k;
-      if (c < h)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) mine[c + e] = acc_pre[k][e];
-    }
+    for (int e = 0; e < 8; ++e) sum[e] = acc_pre[e];
     add_teams(w.pre);
   }
 }
@@ -521,29 +502,43 @@ __global__ __launch_bounds__(kCols* kParts) void gated_norm_reduce_kernel(GatedN
 
 inline size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
+// Calls f with the team width of `lanes` as a compile-time constant.
+template <class F>
+void with_lanes(int lanes, F f) {
+  switch (lanes) {
+    case 8: return f(std::integral_constant<int, 8>{});
+    case 16: return f(std::integral_constant<int, 16>{});
+    case 32: return f(std::integral_constant<int, 32>{});
+    case 64: return f(std::integral_constant<int, 64>{});
+    case 128: return f(std::integral_constant<int, 128>{});
+    case 192: return f(std::integral_constant<int, 192>{});
+    case 256: return f(std::integral_constant<int, 256>{});
+    case 320: return f(std::integral_constant<int, 320>{});
+    case 384: return f(std::integral_constant<int, 384>{});
+    case 448: return f(std::integral_constant<int, 448>{});
+    default: return f(std::integral_constant<int, 512>{});
+  }
+}
+
+constexpr int kFwdRowsMax = 8, kFwdTeams = 4096;
+
 }  // namespace
 
 hipError_t launch_gated_norm_fwd(const GatedNormFwd& p, hipStream_t s) {
   if (p.rows == 0) return hipSuccess;
-  const int waves = team_waves(p.hidden), chunks = (p.hidden + 512 * waves - 1) / (512 * waves);
-  const int64_t per_block = int64_t(4 / waves) * kFwdRows;
-  const unsigned blocks = unsigned((p.rows + per_block - 1) / per_block);
-  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(256), 0, s, p); };
-  auto keep = [&](auto bf16, auto int8, auto e4m3) {
-    if (!p.keep_f && !p.keep_out) launch(bf16);
-    else if (p.format == DCP_ACT_INT8) launch(int8);
-    else launch(e4m3);
-  };
-#define DCP_FWD(W, NC)                                                                            \
-  keep(gated_norm_fwd_kernel<W, NC, DCP_ACT_BF16>, gated_norm_fwd_kernel<W, NC, DCP_ACT_INT8>, \
-       gated_norm_fwd_kernel<W, NC, DCP_ACT_E4M3>)
-  if (waves == 4) DCP_FWD(4, 2);
-  else if (waves == 2 && chunks == 3) DCP_FWD(2, 3);
-  else if (waves == 2) DCP_FWD(2, 2);
-  else if (chunks == 3) DCP_FWD(1, 3);
-  else if (chunks == 2) DCP_FWD(1, 2);
-  else DCP_FWD(1, 1);
-#undef DCP_FWD
+  const int64_t want = p.rows / kFwdTeams;
+  const int team_rows = int(want < 1 ? 1 : want > kFwdRowsMax ? kFwdRowsMax : want);
+  with_lanes(team_lanes(p.hidden), [&](auto tl) {
+    constexpr int TL = decltype(tl)::value;
+    const int64_t per_block = int64_t(Team<TL>::kTeams) * team_rows;
+    const dim3 grid(unsigned((p.rows + per_block - 1) / per_block)), block(Team<TL>::kBlock);
+    if (!p.keep_f && !p.keep_out)
+      hipLaunchKernelGGL((gated_norm_fwd_kernel<TL, DCP_ACT_BF16>), grid, block, 0, s, p, team_rows);
+    else if (p.format == DCP_ACT_INT8)
+      hipLaunchKernelGGL((gated_norm_fwd_kernel<TL, DCP_ACT_INT8>), grid, block, 0, s, p, team_rows);
+    else
+      hipLaunchKernelGGL((gated_norm_fwd_kernel<TL, DCP_ACT_E4M3>), grid, block, 0, s, p, team_rows);
+  });
   return hipGetLastError();
 }
 
@@ -558,31 +553,25 @@ hipError_t launch_gated_norm_bwd(const GatedNormBwd& p, void* workspace, hipStre
   const size_t part = up256(4 * size_t(b.blocks) * size_t(p.hidden));
   const BwdParts w{reinterpret_cast<float*>(ws), reinterpret_cast<float*>(ws + part), reinterpret_cast<float*>(ws + 2 * part),
                    b.team_rows};
-  const int chunks = (p.hidden + 512 * b.waves - 1) / (512 * b.waves);
-  const size_t lds = size_t(4 / b.waves) * p.hidden * sizeof(float);
-  auto launch = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3(unsigned(b.blocks)), dim3(256), lds, s, p, w);
-  };
-  auto pick = [&](auto bf16, auto bf16_32, auto int8, auto int8_32, auto e4m3, auto e4m3_32) {
-    if (p.format == DCP_ACT_BF16) p.dy_f32 ? launch(bf16_32) : launch(bf16);
-    else if (p.format == DCP_ACT_INT8) p.dy_f32 ? launch(int8_32) : launch(int8);
-    else p.dy_f32 ? launch(e4m3_32) : launch(e4m3);
-  };
-#define DCP_BWD(W, NC)                                                                                              \
-  pick(gated_norm_bwd_kernel<W, NC, DCP_ACT_BF16, false>, gated_norm_bwd_kernel<W, NC, DCP_ACT_BF16, true>,       \
-       gated_norm_bwd_kernel<W, NC, DCP_ACT_INT8, false>, gated_norm_bwd_kernel<W, NC, DCP_ACT_INT8, true>,       \
-       gated_norm_bwd_kernel<W, NC, DCP_ACT_E4M3, false>, gated_norm_bwd_kernel<W, NC, DCP_ACT_E4M3, true>)
   if (b.blocks > 0) {
-    if (b.waves == 4) DCP_BWD(4, 2);
-    else if (b.waves == 2 && chunks == 3) DCP_BWD(2, 3);
-    else if (b.waves == 2) DCP_BWD(2, 2);
-    else if (chunks == 3) DCP_BWD(1, 3);
-    else if (chunks == 2) DCP_BWD(1, 2);
-    else DCP_BWD(1, 1);
+    with_lanes(b.lanes, [&](auto tl) {
+      constexpr int TL = decltype(tl)::value;
+      auto launch = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3(unsigned(b.blocks)), dim3(Team<TL>::kBlock), 0, s, p, w);
+      };
+      if (p.format == DCP_ACT_BF16)
+        p.dy_f32 ? launch(gated_norm_bwd_kernel<TL, DCP_ACT_BF16, true>)
+                 : launch(gated_norm_bwd_kernel<TL, DCP_ACT_BF16, false>);
+      else if (p.format == DCP_ACT_INT8)
+        p.dy_f32 ? launch(gated_norm_bwd_kernel<TL, DCP_ACT_INT8, true>)
+                 : launch(gated_norm_bwd_kernel<TL, DCP_ACT_INT8, false>);
+      else
+        p.dy_f32 ? launch(gated_norm_bwd_kernel<TL, DCP_ACT_E4M3, true>)
+                 : launch(gated_norm_bwd_kernel<TL, DCP_ACT_E4M3, false>);
+    });
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-#undef DCP_BWD
   if (!p.dpre && !p.dpost && !p.dgate) return hipSuccess;
   int zs = 0, share = 1;
   if (p.cu) {
