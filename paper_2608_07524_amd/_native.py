@@ -608,19 +608,17 @@ class Layer:
 # ---------------------------------------------------------------------------
 # 8-bit activation checkpoints
 
-def _on_device(call):
-    """Runs a call's launches with its tensors' device as the current one."""
-    def run(torch, device, *args):
-        if device.index is None or device.index == torch.cuda.current_device():
-            return call(torch, device, *args)
-        with torch.cuda.device(device):
-            return call(torch, device, *args)
-    return run
-
-
-@_on_device
 def _enqueue(torch, device, fn, *args):
-    _check(fn(*args, torch.cuda.current_stream(device).cuda_stream))
+    """fn(*args, current stream of ``device``), with ``device`` as the current one."""
+    # (the raw handle: torch.cuda.current_stream builds an object, 2 us a call)
+    stream = torch._C._cuda_getCurrentRawStream(device.index)
+    if device.index == torch._C._cuda_getDevice():
+        st = fn(*args, stream)
+    else:
+        with torch.cuda.device(device):
+            st = fn(*args, stream)
+    if st != DCP_OK:
+        raise DCPError(st, last_error())
 
 
 def _act_dtype(torch, fmt: str):
@@ -649,22 +647,24 @@ def _check_rows(torch, t, name, shape=None):
     """A bf16 [rows, cols] matrix of contiguous rows; returns its row stride."""
     if not hasattr(t, "dim") or t.dim() != 2 or t.dtype != torch.bfloat16:
         raise ValueError(f"{name} must be a bf16 tensor of shape [rows, cols]")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    if t.is_contiguous():
+        return t.shape[1]
     if t.shape[1] > 1 and t.stride(1) != 1:
         raise ValueError(f"{name} must have contiguous rows")
-    return int(t.stride(0)) if t.shape[0] > 1 else int(t.shape[1])
+    return t.stride(0)
 
 
 def _check_codes(torch, codes, scales, shape=None):
     """A checkpoint: contiguous codes [rows, cols] and their uint8 scale bytes."""
     if not hasattr(codes, "dim") or codes.dim() != 2 or not codes.is_contiguous():
         raise ValueError("codes must be a contiguous tensor of shape [rows, cols]")
-    rows, cols = (int(n) for n in codes.shape)
-    if shape is not None and (rows, cols) != tuple(shape):
-        raise ValueError(f"codes have shape {(rows, cols)}, not {tuple(shape)}")
+    rows, cols = codes.shape
+    if shape is not None and codes.shape != shape:
+        raise ValueError(f"codes have shape {tuple(codes.shape)}, not {tuple(shape)}")
     want = (rows, -(-cols // ACT_GROUP))
-    if not hasattr(scales, "dim") or tuple(scales.shape) != want or scales.dtype != torch.uint8 \
+    if not hasattr(scales, "dim") or scales.shape != want or scales.dtype != torch.uint8 \
             or not scales.is_contiguous():
         raise ValueError(f"scales must be a contiguous uint8 tensor of shape {want}")
 
@@ -677,14 +677,15 @@ def act8_pack(x, fmt: str = "int8", codes=None, scales=None):
     import torch
     dtype = _act_dtype(torch, fmt)
     ld = _check_rows(torch, x, "x")
-    rows, cols = (int(n) for n in x.shape)
+    rows, cols = x.shape
     _same_device(x, "x", [(n, t) for n, t in (("codes", codes), ("scales", scales)) if t is not None])
-    codes = torch.empty((rows, cols), dtype=dtype, device=x.device) if codes is None else codes
-    if scales is None:
-        scales = torch.empty((rows, -(-cols // ACT_GROUP)), dtype=torch.uint8, device=x.device)
-    _check_codes(torch, codes, scales, x.shape)
-    if codes.dtype != dtype:
-        raise ValueError(f"codes must be {dtype} for fmt {fmt!r}")
+    given = codes is not None or scales is not None
+    codes = x.new_empty((rows, cols), dtype=dtype) if codes is None else codes
+    scales = x.new_empty((rows, -(-cols // ACT_GROUP)), dtype=torch.uint8) if scales is None else scales
+    if given:
+        _check_codes(torch, codes, scales, x.shape)
+        if codes.dtype != dtype:
+            raise ValueError(f"codes must be {dtype} for fmt {fmt!r}")
     d = Act8DescC(rows, cols, ACT_FORMATS[fmt], ld)
     _enqueue(torch, x.device, load().dcp_act8_pack, d, x.data_ptr(), codes.data_ptr(), scales.data_ptr())
     return codes, scales
@@ -698,9 +699,12 @@ def act8_unpack(codes, scales, out=None):
     if fmt == ACT_BF16:
         raise ValueError("codes must be int8 or float8_e4m3fn")
     _same_device(codes, "codes", [("scales", scales)] + ([("out", out)] if out is not None else []))
-    out = torch.empty(codes.shape, dtype=torch.bfloat16, device=codes.device) if out is None else out
-    ld = _check_rows(torch, out, "out", codes.shape)
-    d = Act8DescC(int(codes.shape[0]), int(codes.shape[1]), fmt, ld)
+    rows, cols = codes.shape
+    if out is None:
+        out, ld = torch.empty_like(codes, dtype=torch.bfloat16), cols
+    else:
+        ld = _check_rows(torch, out, "out", codes.shape)
+    d = Act8DescC(rows, cols, fmt, ld)
     _enqueue(torch, codes.device, load().dcp_act8_unpack, d, codes.data_ptr(), scales.data_ptr(), out.data_ptr())
     return out
 
@@ -720,13 +724,11 @@ def act8_gelu_bwd(codes, scales, da, du=None, a=None):
         raise ValueError("scales go with int8 or float8_e4m3fn codes")
     given = [(n, t) for n, t in (("scales", scales), ("da", da), ("du", du), ("a", a)) if t is not None]
     for n, t in given[1 if scales is not None else 0:]:
-        _check_rows(torch, t, n, codes.shape)
-        if not t.is_contiguous():
-            raise ValueError(f"{n} must be contiguous")
+        _check_matrix(torch, n, t, codes.shape)
     _same_device(codes, "codes", given)
     du = torch.empty_like(da) if du is None else du
     a = torch.empty_like(da) if a is None else a
-    rows, cols = (int(n) for n in codes.shape)
+    rows, cols = codes.shape
     d = Act8DescC(rows, cols, fmt, cols)
     _enqueue(torch, da.device, load().dcp_act8_gelu_bwd, d, codes.data_ptr(), None if scales is None else
              scales.data_ptr(), da.data_ptr(), du.data_ptr(), a.data_ptr())
@@ -766,9 +768,12 @@ def _join_weights(torch, shape, post, gate, pre, cu_seqlens, device):
     """Checks the weights of a join over [rows, hidden]; returns (n_seqs, the
     device tensor of offsets or None)."""
     rows, h = shape
+    on = []
     for name, t in (("post", post), ("pre", pre)):
-        if t is not None and (tuple(t.shape) != (h,) or t.dtype != torch.bfloat16 or not t.is_contiguous()):
-            raise ValueError(f"{name} must be a contiguous bf16 tensor of shape ({h},)")
+        if t is not None:
+            if t.shape != (h,) or t.dtype != torch.bfloat16 or not t.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous bf16 tensor of shape ({h},)")
+            on.append((name, t))
     n = 0
     if cu_seqlens is not None:
         if gate is None:
@@ -781,21 +786,21 @@ def _join_weights(torch, shape, post, gate, pre, cu_seqlens, device):
         elif cu_seqlens.dim() != 1 or cu_seqlens.dtype != torch.int32 or not cu_seqlens.is_contiguous() \
                 or cu_seqlens.numel() < 2:
             raise ValueError("cu_seqlens on a device must be a contiguous int32 tensor of at least two offsets")
-        n = int(cu_seqlens.numel()) - 1
+        n = cu_seqlens.numel() - 1
+        on.append(("cu_seqlens", cu_seqlens))
     if gate is not None:
         want = [(n, h)] if n else [(h,), (1, h)]
-        if tuple(gate.shape) not in want or gate.dtype != torch.bfloat16 or not gate.is_contiguous():
+        if gate.shape not in want or gate.dtype != torch.bfloat16 or not gate.is_contiguous():
             raise ValueError(f"gate must be a contiguous bf16 tensor of shape {want[0]}")
-    _check_on = [(a, t) for a, t in (("post", post), ("gate", gate), ("pre", pre), ("cu_seqlens", cu_seqlens))
-                 if t is not None]
-    for a, t in _check_on:
+        on.append(("gate", gate))
+    for name, t in on:
         if t.device != device:
-            raise ValueError(f"{a} is on {t.device}, the activations on {device}")
+            raise ValueError(f"{name} is on {t.device}, the activations on {device}")
     return n, cu_seqlens
 
 
 def _check_matrix(torch, name, t, shape, dtypes=None):
-    if not hasattr(t, "dim") or tuple(t.shape) != tuple(shape):
+    if not hasattr(t, "dim") or t.shape != shape:
         raise ValueError(f"{name} must be a tensor of shape {tuple(shape)}")
     if t.dtype not in (dtypes or (torch.bfloat16,)) or not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous and bf16" + (" or float32" if dtypes else ""))
@@ -825,18 +830,17 @@ def gated_norm_fwd(x, f, post=None, gate=None, pre=None, cu_seqlens=None, residu
     dtype = None if fmt == "bf16" and keep_f is None and keep_out is None else _act_dtype(torch, fmt)
     _same_device(x, "x", given[1:])
     n, cu = _join_weights(torch, x.shape, post, gate, pre, cu_seqlens, x.device)
-    rows, h = (int(v) for v in x.shape)
+    rows, h = x.shape
     out = torch.empty_like(x) if out is None else out
     if pre is not None and y is None:
         y = torch.empty_like(x)
-    row_scale = lambda on: torch.empty(rows, dtype=torch.float32, device=x.device) if on else None
-    rstd_f, rstd_out = row_scale(post is not None), row_scale(pre is not None)
+    rstd_f = x.new_empty((rows,), dtype=torch.float32) if post is not None else None
+    rstd_out = x.new_empty((rows,), dtype=torch.float32) if pre is not None else None
 
     def kept(on):
         if on is None:
             return None, None
-        t = (torch.empty((rows, h), dtype=dtype, device=x.device),
-             torch.empty((rows, -(-h // ACT_GROUP)), dtype=torch.uint8, device=x.device))
+        t = (x.new_empty((rows, h), dtype=dtype), x.new_empty((rows, -(-h // ACT_GROUP)), dtype=torch.uint8))
         return t, KeptC(t[0].data_ptr(), t[1].data_ptr())
 
     (f8, kf), (out8, ko) = kept(keep_f), kept(keep_out)
@@ -863,7 +867,7 @@ def gated_norm_bwd(dout, dy=None, f=None, out=None, rstd_f=None, rstd_out=None, 
         raise ValueError("dy and y need the gain pre")
     if pre is not None and dy is None:
         raise ValueError("the gain pre needs dy")
-    shape = tuple(int(v) for v in ref.shape)
+    shape = ref.shape
     rows, h = shape
     on = []
     for n_, t in (("dout", dout), ("dx", dx), ("df", df), ("y", y)):
@@ -900,7 +904,7 @@ def gated_norm_bwd(dout, dy=None, f=None, out=None, rstd_f=None, rstd_out=None, 
         raise ValueError("f and out must be kept in one format")
     for n_, t, needed in (("rstd_f", rstd_f, post is not None), ("rstd_out", rstd_out, pre is not None)):
         if needed:
-            if not hasattr(t, "dim") or tuple(t.shape) != (rows,) or t.dtype != torch.float32 or not t.is_contiguous():
+            if not hasattr(t, "dim") or t.shape != (rows,) or t.dtype != torch.float32 or not t.is_contiguous():
                 raise ValueError(f"{n_} must be a contiguous float32 tensor of shape ({rows},)")
             on.append((n_, t))
     if workspace is not None:
@@ -915,16 +919,15 @@ def gated_norm_bwd(dout, dy=None, f=None, out=None, rstd_f=None, rstd_out=None, 
     w = GatedNormPtrsC(_ptr(post), _ptr(gate), _ptr(pre))
     size = C.c_size_t()
     _check(lib.dcp_gated_norm_bwd_workspace_size(d, C.byref(size)))
-    empty = lambda: torch.empty(shape, dtype=torch.bfloat16, device=ref.device)
+    empty = lambda: torch.empty_like(ref, dtype=torch.bfloat16)
     if want_dx and dx is None:
         dx = empty()
     df = empty() if df is None else df
     if want_y and y is None:
         y = empty()
-    grad = lambda t: None if t is None else torch.empty(t.shape, dtype=torch.float32, device=ref.device)
-    dpost, dgate, dpre = grad(post), grad(gate), grad(pre)
+    dpost, dgate, dpre = (None if t is None else torch.empty_like(t, dtype=torch.float32) for t in (post, gate, pre))
     if workspace is None:
-        workspace = torch.empty(size.value, dtype=torch.uint8, device=ref.device)
+        workspace = ref.new_empty((size.value,), dtype=torch.uint8)
     _enqueue(torch, ref.device, lib.dcp_gated_norm_bwd, d, w, _ptr(dout), _ptr(dy), kf, ko, _ptr(rstd_f),
              _ptr(rstd_out), _ptr(dx), df.data_ptr(), _ptr(y), GatedNormPtrsC(_ptr(dpost), _ptr(dgate), _ptr(dpre)),
              workspace.data_ptr(), _nbytes(workspace))

@@ -229,14 +229,18 @@ inline int team_lanes(int hidden) {
   while (l < need) l *= 2;
   return l;
 }
+constexpr int kBwdRowsMax = 32, kBwdBlocks = 768;
 inline BwdShape bwd_shape(int64_t rows, int hidden) {
   BwdShape s;
   s.lanes = team_lanes(hidden);
   s.block = s.lanes > 128 ? s.lanes : 256;
   s.teams_of_block = s.block / s.lanes;
-  // rows of a team: few rows, short chains; many, few partial rows
+  // Rows of a team: at most so many that there are kBwdBlocks workgroups, at most as
+  // many as keep a team's chain of rows and the chains along the partial rows balanced.
   s.team_rows = 1;
-  while (s.team_rows < 64 && int64_t(64) * s.team_rows * s.team_rows < rows) ++s.team_rows;
+  while (s.team_rows < kBwdRowsMax && int64_t(64) * s.team_rows * s.team_rows < rows &&
+         int64_t(s.team_rows) * s.teams_of_block * kBwdBlocks < rows)
+    ++s.team_rows;
   const int64_t per_block = int64_t(s.teams_of_block) * s.team_rows;
   s.blocks = (rows + per_block - 1) / per_block;
   s.teams = s.blocks * s.teams_of_block;
@@ -406,97 +410,137 @@ __global__ __launch_bounds__(Team<TL>::kBlock) void gated_norm_bwd_kernel(GatedN
   }
 }
 
-// Second launch: 32 columns by 32 half-wavefronts a workgroup.  Role 0 adds the
-// workgroups' partial rows of dpre, role 1 those of dpost (and dgate with one gate
-// row); the other roles take sequences, `zs` workgroups along them: each lists those
-// of its share that no team finished, then short ones (up to 32 teams) go one to a
-// half-wavefront, long ones one after another to the whole workgroup.
-constexpr int kCols = 32, kParts = 32, kShareMax = 1024, kSeqBlocks = 64;
-__global__ __launch_bounds__(kCols* kParts) void gated_norm_reduce_kernel(GatedNormBwd p, BwdParts w, int blocks, int zs,
-                                                                          int share) {
+// Second launch, 1024 lanes a workgroup, four kinds of work side by side:
+//  - columns: dpre and dpost (and dgate with one gate row) from the workgroups' partial
+//    rows, 32 columns by 32 parts;
+//  - long: 128 columns of a sequence that goes on for more than kSpan teams behind its
+//    first, 32 half-wavefronts along the teams.  Such a sequence contains the first row of
+//    some kSpan-th team, and the first of these finds it;
+//  - short: one wavefront for each team t and 256 columns, for the sequence, if any,
+//    that starts in t and ends at most kSpan teams later;
+//  - empty: zeros for the sequences without rows.
+// (With a list of the sequences for every 32 columns: 79 us for 4,000 sequences of 1 to
+// 51 tokens, hidden 1,152; long ones one after another in 32 columns: 65 us for 32,768
+// rows of hidden 4,096 in 50 sequences.)
+constexpr int kCols = 32, kParts = 32, kSpan = 32, kLong = 128, kWaves = 16, kWide = 256;
+constexpr int kRuns = 8;  // loads in flight along a column (4 along a short sequence's)
+
+struct ReduceShape {
+  int chunks, strips, wide, long_blocks, short_blocks, empty_blocks;  // 2 * chunks workgroups, then long_blocks, ...
+};
+inline ReduceShape reduce_shape(const BwdShape& b, int hidden, int n_seqs) {
+  ReduceShape r{(hidden + kCols - 1) / kCols, (hidden + kLong - 1) / kLong, (hidden + kWide - 1) / kWide, 0, 0, 0};
+  if (n_seqs == 0) return r;
+  if (b.teams > kSpan) r.long_blocks = int((b.teams + kSpan - 1) / kSpan) * r.strips;
+  r.short_blocks = int((b.teams * r.wide + kWaves - 1) / kWaves);
+  r.empty_blocks = (n_seqs + 1023) / 1024;
+  return r;
+}
+
+__global__ __launch_bounds__(1024) void gated_norm_reduce_kernel(GatedNormBwd p, BwdParts w, ReduceShape g, int blocks) {
   __shared__ float part_sum[kParts][kCols];
-  __shared__ int list[kShareMax], count;
-  const int h = p.hidden, lane = threadIdx.x % kCols, part = threadIdx.x / kCols;
-  const int chunks = (h + kCols - 1) / kCols, role = blockIdx.x / chunks;
-  const int c = (blockIdx.x % chunks) * kCols + lane;
-  // sum of `n` rows of h floats from `src`, stride `stride` rows, over the workgroup
-  auto column = [&](const float* src, int64_t stride, int n) {
-    float s4[4] = {0.f, 0.f, 0.f, 0.f};
-    if (c < h) {
-      int b = part;
-      for (; b + 3 * kParts < n; b += 4 * kParts)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) s4[j] += src[(b + j * kParts) * stride * h + c];
-      for (int j = 0; b < n; b += kParts, ++j) s4[j & 3] += src[b * stride * h + c];
-    }
-    __syncthreads();
-    part_sum[part][lane] = (s4[0] + s4[1]) + (s4[2] + s4[3]);
-    __syncthreads();
-    float t = 0.f;
-    if (part == 0) {
-#pragma unroll
-      for (int q = 0; q < kParts; ++q) t += part_sum[q][lane];
-    }
-    return t;
-  };
+  __shared__ f32x4 long_sum[kParts][kLong / 4];
+  const int h = p.hidden, R = w.team_rows, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   auto put = [&](float* dst, float v) { *dst = p.accumulate ? *dst + v : v; };
   const __bf16 *post = static_cast<const __bf16*>(p.post), *gate = static_cast<const __bf16*>(p.gate);
-  if (role == 0) {
-    if (!p.dpre) return;
-    const float t = column(w.pre, 1, blocks);
-    if (part == 0 && c < h) put(p.dpre + c, t);
-    return;
-  }
-  if (role == 1) {
-    if (!p.dpost && (p.cu || !p.dgate)) return;
-    const float t = column(w.post, 1, blocks);
-    if (part == 0 && c < h) {
-      if (p.dpost) put(p.dpost + c, p.cu || !gate ? t : t * float(gate[c]));
-      if (!p.cu && p.dgate) put(p.dgate + c, post ? t * float(post[c]) : t);
+  int role = blockIdx.x;
+  if (role < 2 * g.chunks) {
+    const int part = threadIdx.x / kCols, col = threadIdx.x % kCols, c = (role >> 1) * kCols + col;
+    const bool pre = (role & 1) == 0;
+    if (pre ? !p.dpre : !p.dpost && (p.cu || !p.dgate)) return;
+    const float* src = pre ? w.pre : w.post;
+    float run[kRuns] = {};
+    if (c < h) {
+      int b = part;
+      for (; b + (kRuns - 1) * kParts < blocks; b += kRuns * kParts)
+#pragma unroll
+        for (int j = 0; j < kRuns; ++j) run[j] += src[int64_t(b + j * kParts) * h + c];
+      for (; b < blocks; b += kParts) run[0] += src[int64_t(b) * h + c];
     }
+#pragma unroll
+    for (int j = kRuns / 2; j > 0; j /= 2)
+#pragma unroll
+      for (int i = 0; i < j; ++i) run[i] += run[i + j];
+    part_sum[part][col] = run[0];
+    __syncthreads();
+    if (part > 0 || c >= h) return;
+    float t = 0.f;
+#pragma unroll
+    for (int q = 0; q < kParts; ++q) t += part_sum[q][col];
+    if (pre) return put(p.dpre + c, t);
+    if (p.dpost) put(p.dpost + c, p.cu || !gate ? t : t * float(gate[c]));
+    if (!p.cu && p.dgate) put(p.dgate + c, post ? t * float(post[c]) : t);
     return;
   }
-  const int z = role - 2, R = w.team_rows;
+  role -= 2 * g.chunks;
   const int64_t rows = min(p.rows, int64_t(p.cu[p.n_seqs]));
-  const float pc = post && c < h ? float(post[c]) : 1.f;
-  for (int64_t base = int64_t(z) * share; base < p.n_seqs; base += int64_t(zs) * share) {
+  // Sequence s as first team, last team and the partial row of the first.
+  struct Span {
+    int64_t t0, t1, head;
+  };
+  auto span = [&](int s) {
+    const int64_t lo = max(int64_t(p.cu[s]), int64_t(0)), hi = min(int64_t(p.cu[s + 1]), rows);
+    Span q{lo / R, (hi - 1) / R, 0};
+    q.head = 2 * q.t0 + (lo % R != 0 ? 1 : 0);
+    return q;
+  };
+  auto partial = [&](int64_t row, int c) { return *reinterpret_cast<const f32x4*>(w.seg + row * h + c); };
+  // Partial rows 2 k, k = k0, k0 + step, ... <= k1.
+  auto along = [&](auto in_flight, int64_t k0, int64_t k1, int64_t step, int c) {
+    constexpr int kN = decltype(in_flight)::value;
+    f32x4 v[kN] = {};
+    int64_t k = k0;
+    for (; k + (kN - 1) * step <= k1; k += kN * step)
+#pragma unroll
+      for (int j = 0; j < kN; ++j) v[j] += partial(2 * (k + j * step), c);
+    for (; k <= k1; k += step) v[0] += partial(2 * k, c);
+#pragma unroll
+    for (int j = kN / 2; j > 0; j /= 2)
+#pragma unroll
+      for (int i = 0; i < j; ++i) v[i] += v[i + j];
+    return v[0];
+  };
+  auto finish = [&](int s, int c, f32x4 v) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) put(p.dgate + int64_t(s) * h + c + e, post ? v[e] * float(post[c + e]) : v[e]);
+  };
+  if (role < g.long_blocks) {
+    const int64_t t = int64_t(role / g.strips) * kSpan;
+    const int part = threadIdx.x / (kLong / 4), col = threadIdx.x % (kLong / 4), c = role % g.strips * kLong + 4 * col;
+    if (t * R >= rows) return;
+    const int s = min(sequence_of<64>(p.cu, p.n_seqs, t * R), p.n_seqs - 1);
+    const Span q = span(s);
+    const int64_t from = q.head - q.t0;  // the first team whose first row it contains
+    if (q.t1 - q.t0 <= kSpan || t < from || t >= from + kSpan) return;
+    long_sum[part][col] =
+        c < h ? along(std::integral_constant<int, kRuns>{}, q.t0 + 1 + part, q.t1, kParts, c) : f32x4{};
     __syncthreads();
-    if (threadIdx.x == 0) count = 0;
-    __syncthreads();
-    const int64_t s = base + threadIdx.x;
-    bool listed = false;
-    if (int(threadIdx.x) < share && s < p.n_seqs) {
-      const int64_t lo = max(int64_t(p.cu[s]), int64_t(0)), hi = min(int64_t(p.cu[s + 1]), rows);
-      if (hi <= lo) {
-        listed = !p.accumulate;  // no rows: the gradient is zero
-      } else {
-        listed = lo / R != (hi - 1) / R;
-      }
-    }
-    if (listed) list[atomicAdd(&count, 1)] = int(s);  // (the order does not reach the results)
-    __syncthreads();
-    const int n = count;
-    for (int i = part; i < n; i += kParts) {
-      const int q = list[i];
-      const int64_t lo = max(int64_t(p.cu[q]), int64_t(0)), hi = min(int64_t(p.cu[q + 1]), rows);
-      const int64_t t0 = lo / R, t1 = hi > lo ? (hi - 1) / R : t0 - 1;
-      if (t1 - t0 >= kParts || c >= h) continue;
-      float v = 0.f;
-      for (int64_t t = t0; t <= t1; ++t) v += w.seg[(2 * t + (t == t0 && lo % R != 0 ? 1 : 0)) * h + c];
-      put(p.dgate + int64_t(q) * h + c, v * pc);
-    }
-    for (int i = 0; i < n; ++i) {
-      const int q = list[i];
-      const int64_t lo = max(int64_t(p.cu[q]), int64_t(0)), hi = min(int64_t(p.cu[q + 1]), rows);
-      const int64_t t0 = lo / R, t1 = hi > lo ? (hi - 1) / R : t0 - 1;
-      if (t1 - t0 < kParts) continue;
-      // the first team's part may lie in slot 1, the others' lie in slot 0
-      float v = column(w.seg + (2 * t0 + 2) * h, 2, int(t1 - t0));
-      if (part == 0 && c < h) {
-        v += w.seg[(2 * t0 + (lo % R != 0 ? 1 : 0)) * h + c];
-        put(p.dgate + int64_t(q) * h + c, v * pc);
-      }
-    }
+    if (part > 0 || c >= h) return;
+    f32x4 v = partial(q.head, c);
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) v += long_sum[k][col];
+    finish(s, c, v);
+    return;
+  }
+  role -= g.long_blocks;
+  if (role < g.short_blocks) {
+    const int64_t unit = int64_t(role) * kWaves + wave, t = unit / g.wide, next = (t + 1) * R;
+    if (next >= rows) return;  // nothing goes on behind team t
+    const int s = min(sequence_of<64>(p.cu, p.n_seqs, next), p.n_seqs - 1);
+    const Span q = span(s);
+    if (q.t0 != t || q.t1 == t || q.t1 - t > kSpan) return;
+    const int c = int(unit % g.wide) * kWide + 4 * lane;
+    if (c < h) finish(s, c, partial(q.head, c) + along(std::integral_constant<int, 4>{}, t + 1, q.t1, 1, c));
+    return;
+  }
+  role -= g.short_blocks;
+  if (p.accumulate) return;
+  const int64_t s = int64_t(role) * 1024 + threadIdx.x;
+  bool none = false;
+  if (s < p.n_seqs) none = min(int64_t(p.cu[s + 1]), rows) <= max(int64_t(p.cu[s]), int64_t(0));
+  for (uint64_t left = __ballot(none); left; left &= left - 1) {
+    float* dst = p.dgate + (s - lane + __ffsll(static_cast<unsigned long long>(left)) - 1) * h;
+    for (int c = lane; c < h; c += 64) dst[c] = 0.f;
   }
 }
 
@@ -520,7 +564,7 @@ void with_lanes(int lanes, F f) {
   }
 }
 
-constexpr int kFwdRowsMax = 8, kFwdTeams = 4096;
+constexpr int kFwdRowsMax = 4, kFwdTeams = 4096;
 
 }  // namespace
 
@@ -573,15 +617,9 @@ hipError_t launch_gated_norm_bwd(const GatedNormBwd& p, void* workspace, hipStre
     if (e != hipSuccess) return e;
   }
   if (!p.dpre && !p.dpost && !p.dgate) return hipSuccess;
-  int zs = 0, share = 1;
-  if (p.cu) {
-    zs = p.n_seqs < kSeqBlocks ? p.n_seqs : kSeqBlocks;
-    share = (p.n_seqs + zs - 1) / zs;
-    share = share < kShareMax ? share : kShareMax;
-  }
-  const unsigned cols = unsigned((p.hidden + kCols - 1) / kCols);
-  hipLaunchKernelGGL(gated_norm_reduce_kernel, dim3(cols * unsigned(2 + zs)), dim3(kCols * kParts), 0, s, p, w,
-                     int(b.blocks), zs, share);
+  const ReduceShape g = reduce_shape(b, p.hidden, p.cu ? p.n_seqs : 0);
+  const unsigned grid = unsigned(2 * g.chunks + g.long_blocks + g.short_blocks + g.empty_blocks);
+  hipLaunchKernelGGL(gated_norm_reduce_kernel, dim3(grid), dim3(1024), 0, s, p, w, g, int(b.blocks));
   return hipGetLastError();
 }
 
