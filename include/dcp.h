@@ -591,12 +591,85 @@ typedef struct {
  * A gate's gradient is summed over its sequence's rows (0 for an empty one), or
  * over all rows where one gate serves all.  Sums are fp32, in an order fixed by rows
  * and hidden: results are bitwise reproducible.  dx or df may be dout's buffer, y, dx
- * or df a bf16 dy's.  Two calls that overlap in time need two workspaces.
+ * or df a bf16 dy's.  The three gradients are distinct buffers.  Two calls that
+ * overlap in time need two workspaces.
  */
 int dcp_gated_norm_bwd(const dcp_gated_norm_desc* desc, const dcp_gated_norm_weights* w, const void* dout,
                        const void* dy, const dcp_kept* f, const dcp_kept* out, const float* rstd_f,
                        const float* rstd_out, void* dx, void* df, void* y, const dcp_gated_norm_grads* grads,
                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Transformer block: the layer with gated, normed joins and a smaller stash */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * The layer above with the joins of its two branches, and with its kept
+ * activations in bf16 or in 8 bits:
+ *   y1 = RMSNorm(x; norm1), q, k, v as there, o = attention(q, k, v),
+ *   h, y2 = join of o Wo into x   (post1, gate1, pre = norm2),
+ *   u = y2 Wup, a = GELU(u),
+ *   out = join of a Wdown into h  (post2, gate2, no pre),
+ * with the join of dcp_gated_norm_fwd: h = residual_scale x + gate1 o RMSNorm(o Wo;
+ * post1).  Without post norms, gates and with residual_scale 1 it is the layer's
+ * function.
+ * The stash holds q, k, v, o, h and u, with post norms or gates also the two
+ * branches' outputs, in stash_format (see dcp_act8_desc), and the LSE and row scales in
+ * fp32: 9 or 11 elements a token and hidden column, where the layer's stash holds 15
+ * in bf16 (y1, y2 and a are formed again in the backward).  An 8-bit stash changes
+ * the gradients by its rounding, not the output; a recomputing backward (stash NULL)
+ * forms everything again in bf16.
+ *   Layout of the stash, each part at the next multiple of 256 bytes: q, k, v, o,
+ * o Wo (with post norms or gates), h, a Wdown (likewise), u -- each bf16, or its codes
+ * and then its scale bytes -- then the LSE [n_heads, T] and 1 / rms of o Wo, h and
+ * a Wdown [T], fp32 (unused ones too).
+ */
+enum { DCP_GATE_NONE = 0, DCP_GATE_SHARED = 1, DCP_GATE_SEQUENCE = 2 };
+
+/*
+ *   layer           as for dcp_layer_fwd (hidden at most 4096, cu_seqlens[n] ==
+ *                   total_tokens).
+ *   stash_format    DCP_ACT_BF16, DCP_ACT_INT8 or DCP_ACT_E4M3.
+ *   post_norm       1: post1 and post2 [hidden] are present.
+ *   gate            DCP_GATE_SHARED: gate1, gate2 [hidden]; DCP_GATE_SEQUENCE:
+ *                   [n_seqs, hidden].
+ *   cu_seqlens      DEVICE copy of the attention descriptor's offsets with
+ *                   DCP_GATE_SEQUENCE, NULL otherwise.
+ *   residual_scale  finite.
+ */
+typedef struct {
+  const dcp_layer_desc* layer;
+  int32_t stash_format;
+  int32_t post_norm;
+  int32_t gate;
+  const int32_t* cu_seqlens;
+  float residual_scale;
+} dcp_block_desc;
+
+/* bf16 device weights; post1, post2, gate1, gate2 where present, else NULL. */
+typedef struct {
+  dcp_layer_weights layer;
+  const void *post1, *gate1, *post2, *gate2;
+} dcp_block_weights;
+
+/* fp32 device gradients of the same shapes; the backward adds into them.  The
+ * matrices' may share buffers, and the vectors of different joins; those of one join
+ * (post1, gate1 and norm2; post2 and gate2) may not. */
+typedef struct {
+  dcp_layer_grads layer;
+  float *post1, *gate1, *post2, *gate2;
+} dcp_block_grads;
+
+/* As dcp_layer_sizes. */
+int dcp_block_sizes(const dcp_block_desc* desc, size_t* stash_bytes, size_t* fwd_workspace_bytes,
+                    size_t* bwd_workspace_bytes);
+
+/* As dcp_layer_fwd and dcp_layer_bwd, on a stash and workspaces of dcp_block_sizes. */
+int dcp_block_fwd(const dcp_block_desc* desc, const dcp_block_weights* w, const void* x, void* out, void* stash,
+                  void* workspace, size_t workspace_bytes, void* stream);
+int dcp_block_bwd(const dcp_block_desc* desc, const dcp_block_weights* w, const void* x, const void* dout, void* dx,
+                  const dcp_block_grads* grads, const void* stash, void* workspace, size_t workspace_bytes,
+                  void* stream);
 
 /* ------------------------------------------------------------------------ */
 /* Schedule replay: DCP against bucket parallelism (Secs. 2.3-2.4, 4.1-4.2)   */

@@ -45,6 +45,7 @@ def pack(x, fmt):
             k[bad] += 1
         scaled = np.where(finite[:, None], part, 0.0) / np.exp2(k.astype(np.float64))[:, None]
         q = np.rint(scaled) if fmt == "int8" else _nearest_e4m3(scaled)
-        vals[:, g * GROUP:(g + 1) * GROUP] = np.where(finite[:, None], q * np.exp2(k.astype(np.float64))[:, None], np.nan)
+        q = q * np.exp2(k.astype(np.float64))[:, None]
+        vals[:, g * GROUP:(g + 1) * GROUP] = np.where(finite[:, None], q, np.nan)
         scales[:, g] = np.where(finite, k + 127, 255)
     return vals, scales

@@ -109,7 +109,17 @@ class KeptC(C.Structure):
     _fields_ = [("data", C.c_void_p), ("scales", C.c_void_p)]
 
 
+class BlockDescC(C.Structure):
+    _fields_ = [("layer", C.POINTER(LayerDescC)), ("stash_format", C.c_int32), ("post_norm", C.c_int32),
+                ("gate", C.c_int32), ("cu_seqlens", C.c_void_p), ("residual_scale", C.c_float)]
+
+
+class BlockWeightsC(C.Structure):
+    _fields_ = [("layer", LayerWeightsC)] + [(n, C.c_void_p) for n in ("post1", "gate1", "post2", "gate2")]
+
+
 ACT_BF16, ACT_INT8, ACT_E4M3 = 0, 1, 2
+GATE_NONE, GATE_SHARED, GATE_SEQUENCE = 0, 1, 2
 ACT_FORMATS = {"bf16": ACT_BF16, "int8": ACT_INT8, "e4m3": ACT_E4M3}
 ACT_GROUP = 32  # columns that share a scale byte
 
@@ -163,6 +173,10 @@ def load() -> C.CDLL:
         "dcp_gated_norm_bwd_workspace_size": ([C.POINTER(GatedNormDescC), C.POINTER(sz)], C.c_int),
         "dcp_gated_norm_bwd": ([C.POINTER(GatedNormDescC), C.POINTER(GatedNormPtrsC), vp, vp, C.POINTER(KeptC),
                                 C.POINTER(KeptC), vp, vp, vp, vp, vp, C.POINTER(GatedNormPtrsC), vp, sz, vp], C.c_int),
+        "dcp_block_sizes": ([C.POINTER(BlockDescC), C.POINTER(sz), C.POINTER(sz), C.POINTER(sz)], C.c_int),
+        "dcp_block_fwd": ([C.POINTER(BlockDescC), C.POINTER(BlockWeightsC), vp, vp, vp, vp, sz, vp], C.c_int),
+        "dcp_block_bwd": ([C.POINTER(BlockDescC), C.POINTER(BlockWeightsC), vp, vp, vp, C.POINTER(BlockWeightsC), vp,
+                           vp, sz, vp], C.c_int),
         "dcp_simulate": ([C.POINTER(C.c_int64), C.c_int32, C.POINTER(C.c_int32), C.c_int32, C.POINTER(CostTableC),
                           C.c_int64, C.POINTER(PlanOptsC), C.POINTER(SimOptsC), C.POINTER(SimResultC),
                           C.POINTER(SimResultC)], C.c_int),
@@ -932,3 +946,116 @@ def gated_norm_bwd(dout, dy=None, f=None, out=None, rstd_f=None, rstd_out=None, 
              _ptr(rstd_out), _ptr(dx), df.data_ptr(), _ptr(y), GatedNormPtrsC(_ptr(dpost), _ptr(dgate), _ptr(dpre)),
              workspace.data_ptr(), _nbytes(workspace))
     return GatedNormGrads(dx, df, y, dpost, dgate, dpre)
+
+
+# ---------------------------------------------------------------------------
+# transformer block
+
+BLOCK_JOINS = ("post1", "gate1", "post2", "gate2")
+
+
+def block_param_shapes(hidden: int, post_norm: bool = False, gates: int = 0):
+    """Shapes of a block's parameters: the layer's, with ``post_norm`` the gains of
+    both branches' output norms, with ``gates`` rows of gates (1, or a row for each
+    sequence) both branches' gates."""
+    h = int(hidden)
+    shapes = dict(layer_param_shapes(h))
+    if post_norm:
+        shapes.update(post1=(h,), post2=(h,))
+    if gates:
+        shapes.update(gate1=(int(gates), h), gate2=(int(gates), h))
+    return shapes
+
+
+class Block:
+    """The layer with gated, normed joins and its stash in ``stash_format`` ("bf16",
+    "int8" or "e4m3"; see dcp_block_fwd / dcp_block_bwd): ``weights`` bf16 and
+    ``grads`` fp32 device tensors keyed as block_param_shapes.  Post norms and gates
+    are there if the weights hold them, both branches' or neither's; gates of n_seqs
+    rows are the sequences' (one row serves all; with one sequence it is the same).
+    ``fwd`` and ``bwd`` as Layer's, on the current stream."""
+
+    def __init__(self, weights, grads, cu_seqlens, n_heads: int, head_dim: int, causal: bool = False,
+                 scale: Optional[float] = None, eps: float = 1e-6, workspace=None, stash_format: str = "bf16",
+                 residual_scale: float = 1.0):
+        import torch
+        self.torch = torch
+        if stash_format not in ACT_FORMATS:
+            raise ValueError(f"stash_format must be one of {tuple(ACT_FORMATS)}, not {stash_format!r}")
+        cu = _host_cu(cu_seqlens)
+        T, n, h = int(cu[-1]), int(cu.size) - 1, n_heads * head_dim
+        self.T, self.hidden = T, h
+        post, gate = "post1" in weights, "gate1" in weights
+        rows = int(weights["gate1"].shape[0]) if gate and weights["gate1"].dim() == 2 else 1
+        if gate and rows not in (1, n):
+            raise ValueError(f"gates have {rows} rows: one, or one for each of {n} sequences")
+        want = block_param_shapes(h, post, rows if gate else 0)
+        dev = weights["wq"].device
+        for what, given, dtype in (("weights", weights, torch.bfloat16), ("grads", grads, torch.float32)):
+            if set(given) != set(want):
+                raise ValueError(f"{what} hold {sorted(given)}, not {sorted(want)}")
+            for name, t in given.items():
+                ok = t.shape == want[name] or (name in ("gate1", "gate2") and rows == 1 and t.shape == (h,))
+                if not ok or t.dtype != dtype or not t.is_contiguous() or t.device != dev:
+                    raise ValueError(f"{what}[{name!r}] must be a contiguous {dtype} tensor of shape {want[name]} "
+                                     f"on {dev}")
+        if not dev.type == "cuda":
+            raise ValueError("tensors must be on a CUDA (HIP) device")
+        self.weights, self.grads = weights, grads
+        self.scale = 1.0 / math.sqrt(head_dim) if scale is None else scale
+        self.d = _Desc(cu, T, n_heads, head_dim, self.scale, causal)
+        self.layer_desc = LayerDescC(C.pointer(self.d.desc), float(eps))
+        kind = GATE_NONE if not gate else GATE_SHARED if rows == 1 else GATE_SEQUENCE
+        self.cu = torch.from_numpy(cu).to(dev) if kind == GATE_SEQUENCE else None
+        self.desc = BlockDescC(C.pointer(self.layer_desc), ACT_FORMATS[stash_format], int(post), kind, _ptr(self.cu),
+                               float(residual_scale))
+        lib = self.lib = load()
+        s, f, b = C.c_size_t(), C.c_size_t(), C.c_size_t()
+        _check(lib.dcp_block_sizes(self.desc, C.byref(s), C.byref(f), C.byref(b)))
+        self.stash_bytes, self.fwd_ws_bytes, self.bwd_ws_bytes = s.value, f.value, b.value
+
+        def pointers(t):
+            return BlockWeightsC(LayerWeightsC(*[t[n].data_ptr() for n in LAYER_PARAMS]),
+                                 *[_ptr(t.get(n)) for n in BLOCK_JOINS])
+
+        self.w, self.g = pointers(weights), pointers(grads)
+        need = max(self.fwd_ws_bytes, self.bwd_ws_bytes)
+        if workspace is not None and (not workspace.is_contiguous() or _nbytes(workspace) < need
+                                      or workspace.device != dev):
+            raise ValueError(f"block workspace needs {need} contiguous bytes on {dev}")
+        # (several blocks of one shape may share one workspace: calls on a stream run in order)
+        self.ws = torch.empty(need, dtype=torch.uint8, device=dev) if workspace is None else workspace
+        self.stash = None
+
+    def _matrix(self, name, t):
+        _check_matrix(self.torch, name, t, (self.T, self.hidden))
+        if t.device != self.ws.device:
+            raise ValueError(f"{name} is on {t.device}, the block on {self.ws.device}")
+
+    def fwd(self, x, keep: bool = True, out=None, stash=None):
+        """``stash``: a preallocated uint8 buffer of stash_bytes to keep into."""
+        t = self.torch
+        out = t.empty_like(x) if out is None else out
+        self._matrix("x", x)
+        self._matrix("out", out)
+        self.stash = None
+        if keep:
+            kept = t.empty(self.stash_bytes, dtype=t.uint8, device=x.device) if stash is None else stash
+            if not kept.is_contiguous() or _nbytes(kept) < self.stash_bytes or kept.device != x.device:
+                raise ValueError(f"the stash needs {self.stash_bytes} contiguous bytes on {x.device}")
+        else:
+            kept = None
+        _enqueue(t, x.device, self.lib.dcp_block_fwd, self.desc, self.w, x.data_ptr(), out.data_ptr(), _ptr(kept),
+                 self.ws.data_ptr(), _nbytes(self.ws))
+        self.stash = kept
+        return out
+
+    def bwd(self, x, dout, dx=None):
+        t = self.torch
+        dx = t.empty_like(x) if dx is None else dx
+        for name, m in (("x", x), ("dout", dout), ("dx", dx)):
+            self._matrix(name, m)
+        _enqueue(t, x.device, self.lib.dcp_block_bwd, self.desc, self.w, x.data_ptr(), dout.data_ptr(), dx.data_ptr(),
+                 self.g, _ptr(self.stash), self.ws.data_ptr(), _nbytes(self.ws))
+        self.stash = None
+        return dx

@@ -25,7 +25,7 @@ PROBE_LIB = os.path.join(PKG, "libdcp_probe.so")
 
 SOURCES = ["attn_fwd.hip", "attn_bwd.hip", "layer.hip", "layer_gemm.hip", "layer_proj.hip", "dcp_api.cpp",
            "dcp_error.cpp", "work_list.cpp", "dcp_plan.cpp", "layer_api.cpp", "noalloc.hip", "act8.hip",
-           "gated_norm.hip", "join_api.cpp"]
+           "gated_norm.hip", "join_api.cpp", "block_api.cpp"]
 
 # Packed fp32 vector ops stay disabled for device code (plain scalar fp32
 # VALU only); the host pass reports the feature as unknown, which is benign.

@@ -437,7 +437,8 @@ inline ReduceShape reduce_shape(const BwdShape& b, int hidden, int n_seqs) {
   return r;
 }
 
-__global__ __launch_bounds__(1024) void gated_norm_reduce_kernel(GatedNormBwd p, BwdParts w, ReduceShape g, int blocks) {
+__global__ __launch_bounds__(1024) void gated_norm_reduce_kernel(GatedNormBwd p, BwdParts w, ReduceShape g,
+                                                                 int blocks) {
   __shared__ float part_sum[kParts][kCols];
   __shared__ f32x4 long_sum[kParts][kLong / 4];
   const int h = p.hidden, R = w.team_rows, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -595,8 +596,8 @@ hipError_t launch_gated_norm_bwd(const GatedNormBwd& p, void* workspace, hipStre
   const BwdShape b = bwd_shape(p.rows, p.hidden);
   char* ws = static_cast<char*>(workspace);
   const size_t part = up256(4 * size_t(b.blocks) * size_t(p.hidden));
-  const BwdParts w{reinterpret_cast<float*>(ws), reinterpret_cast<float*>(ws + part), reinterpret_cast<float*>(ws + 2 * part),
-                   b.team_rows};
+  const BwdParts w{reinterpret_cast<float*>(ws), reinterpret_cast<float*>(ws + part),
+                   reinterpret_cast<float*>(ws + 2 * part), b.team_rows};
   if (b.blocks > 0) {
     with_lanes(b.lanes, [&](auto tl) {
       constexpr int TL = decltype(tl)::value;

@@ -54,7 +54,8 @@ int check_join(const dcp_gated_norm_desc* d, const dcp_gated_norm_weights* w) {
   if (!w) return DCP_OK;
   for (const void* p : {w->post, w->gate, w->pre})
     if (reinterpret_cast<uintptr_t>(p) % 16) return fail(DCP_ERR_INVALID, "weights: not 16-byte aligned");
-  if (d->n_seqs > 0 && !w->gate) return fail(DCP_ERR_INVALID, "cu_seqlens is for a gate of each sequence: gate is null");
+  if (d->n_seqs > 0 && !w->gate)
+    return fail(DCP_ERR_INVALID, "cu_seqlens is for a gate of each sequence: gate is null");
   return DCP_OK;
 }
 
@@ -102,8 +103,8 @@ extern "C" int dcp_act8_unpack(const dcp_act8_desc* d, const void* codes, const 
   return launched(launch_act8_unpack(b, d->format, d->rows, d->cols, d->ld, static_cast<hipStream_t>(stream)));
 }
 
-extern "C" int dcp_act8_gelu_bwd(const dcp_act8_desc* d, const void* codes, const void* scales, const void* da, void* du,
-                                 void* a, void* stream) {
+extern "C" int dcp_act8_gelu_bwd(const dcp_act8_desc* d, const void* codes, const void* scales, const void* da,
+                                 void* du, void* a, void* stream) {
   clear_error();
   DCP_TRY(check_act8(d, true));
   if (d->rows == 0) return DCP_OK;
@@ -182,6 +183,8 @@ extern "C" int dcp_gated_norm_bwd(const dcp_gated_norm_desc* d, const dcp_gated_
   if ((w->post != nullptr) != (g->post != nullptr) || (w->gate != nullptr) != (g->gate != nullptr) ||
       (w->pre != nullptr) != (g->pre != nullptr))
     return fail(DCP_ERR_INVALID, "a gradient goes with each weight");
+  if ((g->post && (g->post == g->gate || g->post == g->pre)) || (g->gate && g->gate == g->pre))
+    return fail(DCP_ERR_INVALID, "two gradients are one buffer");
   for (const float* p : {g->post, g->gate, g->pre})
     if (reinterpret_cast<uintptr_t>(p) % 4) return fail(DCP_ERR_INVALID, "grads: not 4-byte aligned");
   if (d->rows > 0) {  // (buffers of no rows may be null)

@@ -22,58 +22,10 @@
 #include <initializer_list>
 
 #include "dcp_internal.h"
+#include "layer_internal.h"
 #include "layer_launch.h"
 
 namespace dcp {
-namespace {
-
-constexpr size_t kAlign = 256;
-inline size_t up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
-constexpr size_t kGemmWorkspace = size_t(64) << 20;  // rocBLAS scratch, carved from the caller's workspace
-
-constexpr int kMaxHidden = 4096;
-
-struct Dims {
-  int64_t T, H, D, h;
-};
-
-// Activations kept from forward to backward (byte offsets).
-struct Stash {
-  size_t rstd1, y1, q, k, v, o, lse, hres, rstd2, y2, u, a, total;
-};
-Stash stash_layout(const Dims& d) {
-  Stash s{};
-  size_t off = 0;
-  auto take = [&](size_t bytes) {
-    const size_t at = off;
-    off += up(bytes);
-    return at;
-  };
-  const size_t Th = size_t(d.T) * size_t(d.h);
-  s.rstd1 = take(4 * size_t(d.T));
-  s.y1 = take(2 * Th);
-  s.q = take(2 * Th);
-  s.k = take(2 * Th);
-  s.v = take(2 * Th);
-  s.o = take(2 * Th);
-  s.lse = take(4 * size_t(d.H) * size_t(d.T));
-  s.hres = take(2 * Th);
-  s.rstd2 = take(4 * size_t(d.T));
-  s.y2 = take(2 * Th);
-  s.u = take(8 * Th);
-  s.a = take(8 * Th);
-  s.total = off;
-  return s;
-}
-
-// Workspaces: rocBLAS scratch | attention workspace(s) | a stash (used when
-// the caller passes none) | backward temporaries.
-struct FwdWs {
-  size_t gemm, attn, stash, total;
-};
-struct BwdWs {
-  size_t gemm, attn_f, attn_b, stash, da, dy2, dh, dout_recomputed, dq, dk, dv, dy1, partial, total;
-};
 
 int dims_of(const dcp_layer_desc* L, Dims* d) {
   if (!L || !L->attn) return fail(DCP_ERR_INVALID, "layer desc or its attention desc is null");
@@ -90,47 +42,6 @@ int dims_of(const dcp_layer_desc* L, Dims* d) {
   d->h = d->H * d->D;
   // the RMSNorm backward keeps four fp32 rows of gain partials in LDS (<= 64 KB)
   if (d->h > kMaxHidden) return fail(DCP_ERR_UNSUPPORTED, "hidden size %lld exceeds %d", (long long)d->h, kMaxHidden);
-  return DCP_OK;
-}
-
-int fwd_ws(const dcp_layer_desc* L, const Dims& d, FwdWs* w) {
-  size_t na = 0;
-  int st = dcp_varlen_attn_fwd_workspace_size(L->attn, &na);
-  if (st) return st;
-  w->gemm = 0;
-  w->attn = up(kGemmWorkspace);
-  w->stash = w->attn + up(na);
-  w->total = w->stash + stash_layout(d).total;
-  return DCP_OK;
-}
-
-int bwd_ws(const dcp_layer_desc* L, const Dims& d, BwdWs* w) {
-  size_t na = 0, nb = 0;
-  int st = dcp_varlen_attn_fwd_workspace_size(L->attn, &na);
-  if (st) return st;
-  st = dcp_varlen_attn_bwd_workspace_size(L->attn, &nb);
-  if (st) return st;
-  const size_t Th = size_t(d.T) * size_t(d.h);
-  size_t off = up(kGemmWorkspace);
-  auto take = [&](size_t bytes) {
-    const size_t at = off;
-    off += up(bytes);
-    return at;
-  };
-  w->gemm = 0;
-  w->attn_f = take(na);
-  w->attn_b = take(nb);
-  w->stash = take(stash_layout(d).total);
-  w->da = take(8 * Th);  // dA, then dU in place
-  w->dy2 = take(4 * Th);
-  w->dh = take(2 * Th);
-  w->dout_recomputed = take(2 * Th);
-  w->dq = take(2 * Th);
-  w->dk = take(2 * Th);
-  w->dv = take(2 * Th);
-  w->dy1 = take(4 * Th);
-  w->partial = take(4 * size_t(rmsnorm_bwd_blocks(d.T)) * size_t(d.h));
-  w->total = off;
   return DCP_OK;
 }
 
@@ -181,85 +92,97 @@ int gemm(rocblas_handle hd, bool ta, bool tb, int64_t M, int64_t N, int64_t K, c
   return DCP_OK;
 }
 
-// Which projections layer_proj.hip takes.  It saves launches and passes over
-// memory; the library's main loop is faster once the contraction is long, and
-// where its 256-wide tiles fit the hidden size and 192-wide ones do not.
-// Library / fused, us, at (hidden, tokens):
-//   Q, K, V    (1152, 300) 28 / 15, (1152, 16381) 175 / 145, (2048, 1000) 61 /
-//              39, (2048, 4000) 111 / 126, (3072, 1000) 89 / 66, (3072, 8192) 406 / 425
-//   W_up+GELU  (1152, 300) 16 / 17, (1152, 1000) 31 / 22, (1152, 16381) 237 /
-//              201, (2048, 1000) 48 / 51, (2048, 16000) 521 / 543
-//   W_down^T+GELU'  (1152, 300) 14 / 18, (1152, 1000) 27 / 23, (1152, 16381)
-//              249 / 221, (2048, 1000) 47 / 50, (2048, 16000) 522 / 563
-//   dY1        (1152, 1000) 29 / 39, (1152, 2500) 43 / 42, (1152, 16381) 185 /
-//              137, (2048, 4000) 127 / 135
-// Hidden sizes between, inside a step, fused less library at 4,096 / 8,192 /
-// 16,384 / 24,576 tokens:
-//   Q, K, V    1,024 -4 / -4 / +18 / +24; 1,280 -24 / -28 / -37 / +14; 1,536 -18 /
-//              -8 / -17 / -6; 1,664 -21 / -34 / -17 / -41; 1,792 -17 / +7 / +31 / +42
-//   W_up+GELU  1,024 -1 / -7 / +5 / +13; 1,280 -20 / -17 / -16 / -23; 1,536 -16 /
-//              -1 / -7 / -5; 1,664 -5 / -3 / -1 / +1; 1,792 -3 / -14 / +5 / -33
-//   W_down^T+GELU'  1,024 +5 / +3 / +7 / +18; 1,280 -8 / -28 / +18 / +45; 1,536 -3 /
-//              +6 / +8 / +15; 1,664 +5 / 0 / +6 / +37; 1,792 +3 / -12 / +60 / -19
-//   dY1        1,024 -6 / -13 / -8 / -20; 1,536 -6 / -13 / -30 / -48; 1,792 +3 / -2 /
-//              +18 / -41
-constexpr int64_t kProjHidden = 1536;
-constexpr int64_t kProjTile = 192;
-inline int64_t proj_tiles(int64_t n) { return (n + kProjTile - 1) / kProjTile; }
-// (1,024 and smaller powers of two: 192-wide tiles pad them by an eighth or more)
-inline bool library_width(const Dims& d) {
-  return d.h % 256 == 0 && 10 * kProjTile * proj_tiles(d.h) > 11 * d.h && d.T * d.h > int64_t(12) << 20;
-}
-inline bool fused_qkv(const Dims& d) {
-  return (d.h <= kProjHidden && !library_width(d)) || d.T * d.h <= int64_t(4) << 20;
-}
-inline bool fused_gelu(const Dims& d) { return d.h <= kProjHidden && d.T >= 512 && !library_width(d); }
-inline bool fused_dy1(const Dims& d) { return d.h <= kProjHidden && d.T >= 2048; }
-// W_o with its residual and dO (contraction h), W_down with its residual (4 h),
-// from 6,144 tokens; below, the library is a little faster.  Where the host's
-// enqueueing bounds the step (hidden 256, 6,144 tokens: 73 us forward) all three
-// save a library call's 10 to 13 us of it.  Otherwise W_o and dO, if the library's
-// 256-wide tiles do not divide the hidden size and the last round of 512 workgroups
-// (two per CU) is mostly full.  Fused less library, change of the forward by W_o and
-// of the step by dO: 108 sizes within the rule (768 to 1,472 wide, 6,144 to 28,672
-// tokens) -1.2 % (worst +2.3, best -5) and -0.3 %; hidden 1,152: 336 tiles (0.66 of
-// a round) +7.9 us of 310, 384 (0.75) -4.7 of 385, 768 -16.5 of 710, 1,152 -17 of
-// 1,020; multiples of 256: 1,024 +4 to +26, 1,536 -18 to +20.  W_down is the
-// library's: +10 to +60 us at most sizes (1,152 wide: 10,240 tokens +5, 12,288 +34,
-// 24,576 +10; 1,440: +11 to +62), -25 only around 768 tiles of hidden 1,152.
-constexpr int64_t kPlainTokens = 6144;
-inline bool enqueue_bound(const Dims& d) { return d.T >= kPlainTokens && d.T * d.h <= int64_t(2) << 20; }
-inline bool fused_square(const Dims& d) {
-  const int64_t tiles = (d.T + 127) / 128 * proj_tiles(d.h), rounds = (tiles + 511) / 512;
-  return enqueue_bound(d) || (d.h <= kProjHidden && d.h % 256 != 0 && d.T >= kPlainTokens && 10 * tiles >= 7 * 512 * rounds);
-}
-
-// The weight gradients are the library's at hidden size 4,096, the largest, with
-// many tokens: its tiles divide 4,096, 192-wide ones pad each side by 3 %.  One
-// launch of all six less six products, change of the step: 4,096 at 2,048 / 8,192 /
-// 10,240 / 12,288 / 16,384 / 32,768 tokens -2.0 / +0.1 / -0.9 / +0.6 to +2.3 / +1.4
-// to +2.8 / +3.3 %; 2,048 (as much padding) -4.1 / -4.9 / - / -5.7 / -4.8 / -0.9,
-// 3,840 -4.3 / -6.6 / - / -4.6 / -4.2 / -4.6.
-inline bool library_wgrad(const Dims& d) { return d.h >= 4096 && d.T >= 12288; }
-
 int check_ptrs(std::initializer_list<const void*> ps, const char* what) {
   for (const void* p : ps)
     if (!p || reinterpret_cast<uintptr_t>(p) % 16) return fail(DCP_ERR_INVALID, "%s: null or not 16-byte aligned", what);
   return DCP_OK;
 }
 
-inline char* at(void* base, size_t off) { return static_cast<char*>(base) + off; }
+int check_weights(const dcp_layer_weights* w) {
+  if (!w) return fail(DCP_ERR_INVALID, "weights are null");
+  return check_ptrs({w->norm1, w->wq, w->wk, w->wv, w->wo, w->norm2, w->w_up, w->w_down}, "weights");
+}
 
-#define DCP_TRY(x)          \
-  do {                      \
-    int st_ = (x);          \
-    if (st_) return st_;    \
-  } while (0)
-#define DCP_HIP(x)                                                                          \
-  do {                                                                                      \
-    hipError_t e_ = (x);                                                                    \
-    if (e_ != hipSuccess) return fail(DCP_ERR_HIP, "layer kernel: %s", hipGetErrorString(e_)); \
-  } while (0)
+namespace {
+
+// Activations kept from forward to backward (byte offsets).
+struct Stash {
+  size_t rstd1, y1, q, k, v, o, lse, hres, rstd2, y2, u, a, total;
+};
+Stash stash_layout(const Dims& d) {
+  Stash s{};
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off += up(bytes);
+    return at;
+  };
+  const size_t Th = size_t(d.T) * size_t(d.h);
+  s.rstd1 = take(4 * size_t(d.T));
+  s.y1 = take(2 * Th);
+  s.q = take(2 * Th);
+  s.k = take(2 * Th);
+  s.v = take(2 * Th);
+  s.o = take(2 * Th);
+  s.lse = take(4 * size_t(d.H) * size_t(d.T));
+  s.hres = take(2 * Th);
+  s.rstd2 = take(4 * size_t(d.T));
+  s.y2 = take(2 * Th);
+  s.u = take(8 * Th);
+  s.a = take(8 * Th);
+  s.total = off;
+  return s;
+}
+
+// Workspaces: rocBLAS scratch | attention workspace(s) | a stash (used when
+// the caller passes none) | backward temporaries.
+struct FwdWs {
+  size_t gemm, attn, stash, total;
+};
+struct BwdWs {
+  size_t gemm, attn_f, attn_b, stash, da, dy2, dh, dout_recomputed, dq, dk, dv, dy1, partial, total;
+};
+
+int fwd_ws(const dcp_layer_desc* L, const Dims& d, FwdWs* w) {
+  size_t na = 0;
+  int st = dcp_varlen_attn_fwd_workspace_size(L->attn, &na);
+  if (st) return st;
+  w->gemm = 0;
+  w->attn = up(kGemmWorkspace);
+  w->stash = w->attn + up(na);
+  w->total = w->stash + stash_layout(d).total;
+  return DCP_OK;
+}
+
+int bwd_ws(const dcp_layer_desc* L, const Dims& d, BwdWs* w) {
+  size_t na = 0, nb = 0;
+  int st = dcp_varlen_attn_fwd_workspace_size(L->attn, &na);
+  if (st) return st;
+  st = dcp_varlen_attn_bwd_workspace_size(L->attn, &nb);
+  if (st) return st;
+  const size_t Th = size_t(d.T) * size_t(d.h);
+  size_t off = up(kGemmWorkspace);
+  auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off += up(bytes);
+    return at;
+  };
+  w->gemm = 0;
+  w->attn_f = take(na);
+  w->attn_b = take(nb);
+  w->stash = take(stash_layout(d).total);
+  w->da = take(8 * Th);  // dA, then dU in place
+  w->dy2 = take(4 * Th);
+  w->dh = take(2 * Th);
+  w->dout_recomputed = take(2 * Th);
+  w->dq = take(2 * Th);
+  w->dk = take(2 * Th);
+  w->dv = take(2 * Th);
+  w->dy1 = take(4 * Th);
+  w->partial = take(4 * size_t(rmsnorm_bwd_blocks(d.T)) * size_t(d.h));
+  w->total = off;
+  return DCP_OK;
+}
 
 // The forward into stash buffers `s` (offsets from `sb`), output `out`.
 int forward(const dcp_layer_desc* L, const Dims& d, const dcp_layer_weights* w, const void* x, void* out, void* sb,
@@ -297,11 +220,6 @@ int forward(const dcp_layer_desc* L, const Dims& d, const dcp_layer_weights* w, 
   }
   DCP_TRY(add(enqueue_bound(d), at(sb, s.a), w->w_down, at(sb, s.hres), out, 4 * h));
   return DCP_OK;
-}
-
-int check_weights(const dcp_layer_weights* w) {
-  if (!w) return fail(DCP_ERR_INVALID, "weights are null");
-  return check_ptrs({w->norm1, w->wq, w->wk, w->wv, w->wo, w->norm2, w->w_up, w->w_down}, "weights");
 }
 
 }  // namespace

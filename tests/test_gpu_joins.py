@@ -109,8 +109,8 @@ def test_pack_and_unpack(torch, P, fmt, rows, cols, ld):
     assert np.array_equal(np.where(np.isinf(want), np.copysign(2.0 ** 128, want), want), vals, equal_nan=True)
     assert np.array_equal(_f64(back), want, equal_nan=True)
     # (NaN groups hold codes 0)
-    held = np.where(np.isnan(vals), 0.0, vals) / np.repeat(np.exp2(scales.astype(np.float64) - 127), 32, axis=1)[:, :cols]
-    assert np.array_equal(codes.float().cpu().numpy(), np.where(np.isnan(vals), 0.0, held))
+    held = np.where(np.isnan(vals), 0.0, vals / np.repeat(np.exp2(scales.astype(np.float64) - 127), 32, axis=1)[:, :cols])
+    assert np.array_equal(codes.float().cpu().numpy(), held)
     if ld > cols:  # into a slice: the columns beside it stay
         out = torch.full((rows, ld), 7.0, dtype=torch.bfloat16, device="cuda")
         P.act8_unpack(codes, s, out=out[:, :cols])
@@ -169,7 +169,8 @@ def test_checkpoints_of_more_than_2_31_elements(torch, P):
 def test_no_rows(torch, P):
     x = torch.empty(0, 64, dtype=torch.bfloat16, device="cuda")
     codes, s = P.act8_pack(x)
-    assert tuple(codes.shape) == (0, 64) and tuple(s.shape) == (0, 2) and tuple(P.act8_unpack(codes, s).shape) == (0, 64)
+    assert tuple(codes.shape) == (0, 64) and tuple(s.shape) == (0, 2)
+    assert tuple(P.act8_unpack(codes, s).shape) == (0, 64)
     g = torch.ones(64, dtype=torch.bfloat16, device="cuda")
     r = P.gated_norm_fwd(x, x, g, g, g)
     b = P.gated_norm_bwd(x, x, x, x, r.rstd_f, r.rstd_out, g, g, g)
@@ -209,7 +210,8 @@ def _case(torch, P, lengths, h, gate, post, pre, fmt, f32, alpha=1.0, extra=0, s
     keep = {} if fmt == "bf16" else dict(keep_f=fmt, **(dict(keep_out=fmt) if pre else {}))
     mark = lambda: torch.full((rows, h), 7.0, dtype=torch.bfloat16, device="cuda")
     kept = lambda t: bool((t[T:] == 7.0).all())
-    r = P.gated_norm_fwd(x, f, cu_seqlens=cu_t, residual_scale=alpha, out=mark(), y=mark() if pre else None, **wt, **keep)
+    r = P.gated_norm_fwd(x, f, cu_seqlens=cu_t, residual_scale=alpha, out=mark(), y=mark() if pre else None, **wt,
+                         **keep)
     o = J.forward(x64, f64, cu=per, alpha=alpha, **w64)
     gates = J._gate_rows(w64.get("gate"), per, T)
     n = f64 if not post else f64 * o["rstd_f"][:, None] * w64["post"]

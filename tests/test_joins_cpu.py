@@ -128,7 +128,8 @@ def _join(rows=8, hidden=64, n_seqs=0, cu=None, alpha=1.0, eps=1e-6, fmt=N.ACT_B
 @pytest.mark.parametrize("kw,code", [
     (dict(rows=-1), N.DCP_ERR_INVALID), (dict(rows=1 << 31), N.DCP_ERR_INVALID), (dict(hidden=0), N.DCP_ERR_INVALID),
     (dict(hidden=60), N.DCP_ERR_UNSUPPORTED), (dict(hidden=4104), N.DCP_ERR_UNSUPPORTED),
-    (dict(n_seqs=2), N.DCP_ERR_INVALID), (dict(cu=FAKE), N.DCP_ERR_INVALID), (dict(n_seqs=-1, cu=FAKE), N.DCP_ERR_INVALID),
+    (dict(n_seqs=2), N.DCP_ERR_INVALID), (dict(cu=FAKE), N.DCP_ERR_INVALID),
+    (dict(n_seqs=-1, cu=FAKE), N.DCP_ERR_INVALID),
     (dict(n_seqs=2, cu=FAKE + 2), N.DCP_ERR_INVALID), (dict(alpha=float("inf")), N.DCP_ERR_INVALID),
     (dict(eps=-1.0), N.DCP_ERR_INVALID), (dict(eps=float("nan")), N.DCP_ERR_INVALID), (dict(fmt=3), N.DCP_ERR_INVALID),
     (dict(f32=2), N.DCP_ERR_INVALID), (dict(acc=-1), N.DCP_ERR_INVALID),
@@ -173,20 +174,23 @@ def test_join_backward_refusals():
     assert lib.dcp_gated_norm_bwd_workspace_size(C.byref(d), C.byref(n)) == 0 and n.value >= 2 * 4 * 64
     assert lib.dcp_gated_norm_bwd_workspace_size(C.byref(d), None) == N.DCP_ERR_INVALID
     w, k = N.GatedNormPtrsC(FAKE, FAKE, FAKE), N.KeptC(FAKE, FAKE)
+    grads = N.GatedNormPtrsC(FAKE, FAKE + 256, FAKE + 512)
 
-    def call(wt=w, dout=FAKE, dy=FAKE, f=k, out=k, rf=FAKE, ro=FAKE, dx=FAKE, df=2 * FAKE, y=None, g=w, ws=FAKE,
+    def call(wt=w, dout=FAKE, dy=FAKE, f=k, out=k, rf=FAKE, ro=FAKE, dx=FAKE, df=2 * FAKE, y=None, g=grads, ws=FAKE,
              size=n.value):
         ref = lambda s: None if s is None else C.byref(s)
-        return lib.dcp_gated_norm_bwd(C.byref(d), ref(wt), dout, dy, ref(f), ref(out), rf, ro, dx, df, y, ref(g), ws, size,
-                                      None)
+        return lib.dcp_gated_norm_bwd(C.byref(d), ref(wt), dout, dy, ref(f), ref(out), rf, ro, dx, df, y, ref(g), ws,
+                                      size, None)
 
     bad = N.DCP_ERR_INVALID
     for kw in (dict(wt=None), dict(g=None), dict(dy=None), dict(dy=FAKE + 4), dict(dout=FAKE + 8), dict(f=None),
                dict(out=None), dict(f=N.KeptC(FAKE, None)), dict(out=N.KeptC(FAKE + 1, FAKE)), dict(rf=None),
                dict(ro=None), dict(df=None), dict(dx=2 * FAKE), dict(y=FAKE), dict(y=FAKE + 8),
-               dict(g=N.GatedNormPtrsC(FAKE, None, FAKE)), dict(g=N.GatedNormPtrsC(FAKE, FAKE, FAKE + 1)),
-               dict(wt=N.GatedNormPtrsC(FAKE, FAKE, None), g=N.GatedNormPtrsC(FAKE, FAKE, None)),  # dy without pre
-               dict(wt=N.GatedNormPtrsC(FAKE, FAKE, None), g=N.GatedNormPtrsC(FAKE, FAKE, None), dy=None, dout=None)):
+               dict(g=N.GatedNormPtrsC(FAKE, None, 2 * FAKE)), dict(g=N.GatedNormPtrsC(FAKE, 2 * FAKE, FAKE + 1)),
+               dict(g=N.GatedNormPtrsC(FAKE, FAKE, 2 * FAKE)), dict(g=N.GatedNormPtrsC(FAKE, 2 * FAKE, 2 * FAKE)),
+               dict(wt=N.GatedNormPtrsC(FAKE, FAKE, None), g=N.GatedNormPtrsC(FAKE, 2 * FAKE, None)),  # dy without pre
+               dict(wt=N.GatedNormPtrsC(FAKE, FAKE, None), g=N.GatedNormPtrsC(FAKE, 2 * FAKE, None), dy=None,
+                    dout=None)):
         assert call(**kw) == bad, kw
     for kw in (dict(ws=None), dict(ws=FAKE + 16), dict(size=n.value - 1)):
         assert call(**kw) == N.DCP_ERR_WORKSPACE, kw
