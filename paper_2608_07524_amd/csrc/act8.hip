@@ -61,18 +61,6 @@ __global__ __launch_bounds__(256) void act8_unpack_kernel(ActBatch b, Pieces d) 
   *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(b.dst[m]) + at.wide) = o;
 }
 
-// GELU, tanh form, through the logistic function: with w = k0 (u + k1 u^3),
-// (1 + tanh w) / 2 = s(2w) = 1 / (1 + e^(-2w)), so a = u s and
-// da/du = s + 2 k0 u s (1 - s) (1 + 3 k1 u^2).  s is 0 or 1 in fp32 beyond |u| = 16,
-// where the powers of u are cut so that they stay finite.
-__device__ __forceinline__ void gelu_and_slope(float u, float* a, float* slope) {
-  constexpr float k0 = 0.7978845608028654f, k1 = 0.044715f, log2e = 1.4426950408889634f;
-  const float c = fminf(fmaxf(u, -16.f), 16.f), cc = c * c;
-  const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-2.f * k0 * log2e * c * (1.f + k1 * cc)));
-  *a = u * s;
-  *slope = s + u * (s * (1.f - s) * (2.f * k0 + 6.f * k0 * k1 * cc));
-}
-
 template <int FMT, bool DENSE>
 __global__ __launch_bounds__(256) void act_gelu_bwd_kernel(const void* u, const uint8_t* scales, const __bf16* da,
                                                            __bf16* du, __bf16* a, Pieces d) {

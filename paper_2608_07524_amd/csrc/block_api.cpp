@@ -8,9 +8,9 @@
 // the row scales.  y1, y2 and a, which the layer keeps as well, come out of passes
 // that the backward makes anyway (a from the activation's, y2 from the join's) or of
 // one short one (y1).  The forward writes the checkpoints of f1, h and f2 in the
-// joins' own passes and packs q, k, v and o in one launch and u in another; the
-// backward's joins and activation read theirs in place, and one launch brings q, k, v
-// and o back for the attention.
+// joins' own passes, that of u in W_up's (where the kernel of layer_proj.hip forms
+// it), and packs q, k, v and o in one launch; the backward's joins and activation read
+// theirs in place, and one launch brings q, k, v and o back for the attention.
 #include <hip/hip_runtime.h>
 #include <rocblas/rocblas.h>
 
@@ -149,6 +149,19 @@ struct Acts {
   float *lse, *rstd_f1, *rstd_h, *rstd_f2;
 };
 
+// W_up with GELU (and u's checkpoint) is one kernel of layer_proj.hip at every token
+// count, W_down^T with GELU' and GELU one where u is kept in bf16 and the layer's rule
+// takes it.  One kernel less the library's product and the passes behind it, us:
+//   W_up, u in 8 bits  (128, 429) -18, (1152, 300) -4, (1152, 1000) -14, (1152, 4096)
+//              -23, (1152, 16381) -71, (1024, 16384) -36, (1536, 8192) -37, (1792,
+//              8192) +4, (4096, 4096) +47
+//   W_up, u in bf16    -16, -3, -13, -9, -20, -18, -11, +20, +72 (the rule is the same, so
+//              that the output does not depend on the stash)
+//   W_down^T, bf16     (256, 2048) -3, (1152, 1000) -3, (1152, 4096) -25, (1152, 16381)
+//              -36, (1024, 4096) +8, (1536, 8192) +4, (2048, 4096) +13
+//   W_down^T, 8 bits   -2, -2, -10, +29, +20, +34, +30: not taken
+inline bool fused_up(const Dims& d) { return d.h <= kProjHidden; }
+
 // Activations in bf16 at `base`, in kept_layout's places; f1 and f2, where it has
 // none, behind them.
 Acts acts_in(const Block& b, void* base) {
@@ -244,16 +257,18 @@ int forward(const dcp_block_desc* desc, const Block& b, const dcp_block_weights*
   j.alpha = desc->residual_scale;
   j.eps = desc->layer->eps;
   DCP_HIP(launch_gated_norm_fwd(j, st));
-  if (fused_gelu(d)) {
-    const Proj p{{y2}, {lw.w_up}, {s.bf16[kU]}, nullptr, a, T, int(4 * h), int(h), 1, 1, 0};
-    DCP_HIP(launch_proj(p, ProjEpilogue::kGelu, st));
+  const bool keep_u = s.kept[kU].data != nullptr;
+  if (fused_up(d)) {
+    const Proj p{{y2}, {lw.w_up}, {keep_u ? s.kept[kU].data : s.bf16[kU]}, nullptr, a, T, int(4 * h), int(h), 1, 1, 0,
+                 b.format, s.kept[kU].scales};
+    DCP_HIP(launch_proj(p, keep_u ? ProjEpilogue::kGeluKeep : ProjEpilogue::kGelu, st));
   } else {
     DCP_TRY(gemm(hd, false, false, T, 4 * h, h, y2, lw.w_up, 0.f, s.bf16[kU], s.bf16[kU], false));
     DCP_HIP(launch_gelu_fwd(s.bf16[kU], a, T * 4 * h, st));
-  }
-  if (s.kept[kU].data) {
-    const ActBatch p{{s.bf16[kU]}, {s.kept[kU].data}, {s.kept[kU].scales}, 1};
-    DCP_HIP(launch_act8_pack(p, b.format, T, int(4 * h), 4 * h, st));
+    if (keep_u) {
+      const ActBatch p{{s.bf16[kU]}, {s.kept[kU].data}, {s.kept[kU].scales}, 1};
+      DCP_HIP(launch_act8_pack(p, b.format, T, int(4 * h), 4 * h, st));
+    }
   }
   DCP_TRY(gemm(hd, false, false, T, h, 4 * h, a, lw.w_down, 0.f, s.bf16[kF2], s.bf16[kF2], false));
   j.x = s.bf16[kH];
@@ -407,8 +422,13 @@ extern "C" int dcp_block_bwd(const dcp_block_desc* desc, const dcp_block_weights
   }
   // MLP: dA = dF2 Wdown^T; dU = dA GELU'(U) in place, A = GELU(U)
   void* da = at(workspace, v.da);
-  DCP_TRY(gemm(hd, false, true, T, 4 * h, h, df2, lw.w_down, 0.f, da, da, false));
-  DCP_HIP(launch_act_gelu_bwd(s.kept[kU].data, s.kept[kU].scales, format, da, da, a, T, int(4 * h), 4 * h, st));
+  if (format == DCP_ACT_BF16 && fused_gelu(d)) {
+    const Proj p{{df2}, {lw.w_down}, {da}, s.bf16[kU], a, T, int(4 * h), int(h), 1, 1, 0, format, nullptr};
+    DCP_HIP(launch_proj(p, ProjEpilogue::kGeluBack, st));
+  } else {
+    DCP_TRY(gemm(hd, false, true, T, 4 * h, h, df2, lw.w_down, 0.f, da, da, false));
+    DCP_HIP(launch_act_gelu_bwd(s.kept[kU].data, s.kept[kU].scales, format, da, da, a, T, int(4 * h), 4 * h, st));
+  }
   // dY2 = dU Wup^T (fp32), then the attention's join: gradients of f1 and x, and Y2
   void* dY2 = at(workspace, v.f32);
   DCP_TRY(gemm(hd, false, true, T, h, 4 * h, da, lw.w_up, 0.f, dY2, dY2, true));

@@ -42,6 +42,8 @@ enum class ProjEpilogue {
   kGeluGrad,  // a w^T times GELU'(aux), bf16
   kStoreT,    // a w^T, bf16
   kSumF32,    // sum of a w^T, fp32
+  kGeluKeep,  // the 8-bit checkpoint of a w (rounded to bf16), and GELU of it to out2
+  kGeluBack,  // a w^T times GELU'(aux), bf16, and GELU(aux) to out2
 };
 constexpr int kProjMax = 3;
 struct Proj {
@@ -53,6 +55,8 @@ struct Proj {
   int64_t tokens;
   int n, k, pairs, outs;
   int n_tiles;  // (set by the launch)
+  int format;   // kGeluKeep: DCP_ACT_INT8 or _E4M3 codes to out[0] and their bytes to scales (n a multiple of 32)
+  void* scales;
 };
 hipError_t launch_proj(const Proj& p, ProjEpilogue epi, hipStream_t s);
 

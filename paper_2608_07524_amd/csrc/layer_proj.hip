@@ -1,8 +1,9 @@
 // Projections of the transformer layer: C[T, N] = sum_s A_s W_s (or A_s W_s^T)
 // over up to three operand pairs of the same shape, A [T, K] and W ([K, N], or
 // [N, K] when transposed) bf16 row-major, with what follows a projection in the
-// layer done on the accumulators: the residual, GELU and its derivative, or the
-// plain fp32 sum the RMSNorm backward reads.  Q, K and V are one launch (three
+// layer done on the accumulators: the residual, GELU (its argument in bf16 or as an
+// 8-bit checkpoint) and its derivative, or the plain fp32 sum the RMSNorm backward
+// reads.  Q, K and V are one launch (three
 // outputs), and so is dY1 = dQ Wq^T + dK Wk^T + dV Wv^T (one sum).
 //
 // Tiles of 192 features x 64 * TB tokens, four wavefronts in 2 x 2, each with
@@ -19,6 +20,7 @@
 // the rules in layer_api.cpp.
 #include <type_traits>
 
+#include "act8.h"
 #include "attn_common.h"
 #include "layer_launch.h"
 
@@ -131,7 +133,8 @@ __device__ __forceinline__ float gelu_grad(float u) {
   return fmaf(u * (s * (1.f - s)), 2.f * kGeluK0 * fmaf(3.f * kGeluK1 * u, u, 1.f), s);
 }
 
-template <bool WT, int TB, ProjEpilogue EPI>
+// FMT: format of the checkpoint that kGeluKeep writes.
+template <bool WT, int TB, ProjEpilogue EPI, int FMT>
 __global__ __launch_bounds__(kThreads, 2) void proj_kernel(Proj p) {
   constexpr int TT = 64 * TB;  // tokens per tile
   using XS = RowSlice<TT>;
@@ -208,7 +211,8 @@ __global__ __launch_bounds__(kThreads, 2) void proj_kernel(Proj p) {
   // Half the tokens of the output at a time, eight features per thread and item;
   // what the epilogue reads (GELU's argument, the residual) is fetched before the products.
   constexpr int kItems = HALF * kWChunks / kThreads;
-  constexpr bool kAux = EPI == ProjEpilogue::kGeluGrad || EPI == ProjEpilogue::kResidual;
+  constexpr bool kBack = EPI == ProjEpilogue::kGeluBack;
+  constexpr bool kAux = kBack || EPI == ProjEpilogue::kGeluGrad || EPI == ProjEpilogue::kResidual;
   bf16x8 aux[kAux ? 2 : 1][kItems];
   if constexpr (kAux) {
 #pragma unroll
@@ -296,6 +300,17 @@ __global__ __launch_bounds__(kThreads, 2) void proj_kernel(Proj p) {
         f32x4* out = reinterpret_cast<f32x4*>(static_cast<float*>(p.out[0]) + at);
         out[0] = lo;
         out[1] = hi;
+      } else if constexpr (kBack) {
+        bf16x8 r, a;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float act, slope;
+          gelu_and_slope(float(aux[hm][n][e]), &act, &slope);
+          r[e] = __bf16((e < 4 ? lo[e] : hi[e - 4]) * slope);
+          a[e] = __bf16(act);
+        }
+        *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.out[0]) + at) = r;
+        *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.out2) + at) = a;
       } else {
         bf16x8 r;
 #pragma unroll
@@ -305,8 +320,15 @@ __global__ __launch_bounds__(kThreads, 2) void proj_kernel(Proj p) {
           if constexpr (EPI == ProjEpilogue::kGeluGrad) v *= gelu_grad(float(aux[hm][n][e]));
           r[e] = __bf16(v);
         }
-        *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.out[pl.out]) + at) = r;
-        if constexpr (EPI == ProjEpilogue::kGelu) {
+        if constexpr (EPI == ProjEpilogue::kGeluKeep) {
+          // (a group's four lanes have one row and N is a multiple of 32: all or none are here)
+          const uint32_t byte = scale_byte<FMT>(group_top(top_bits(r)));
+          *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(p.out[0]) + at) = encode8<FMT>(r, byte);
+          if (c % 4 == 0) static_cast<uint8_t*>(p.scales)[int64_t(row) * (N / kActGroup) + col / kActGroup] = uint8_t(byte);
+        } else {
+          *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.out[pl.out]) + at) = r;
+        }
+        if constexpr (EPI == ProjEpilogue::kGelu || EPI == ProjEpilogue::kGeluKeep) {
           bf16x8 a;
 #pragma unroll
           for (int e = 0; e < 8; ++e) a[e] = __bf16(gelu(float(r[e])));
@@ -317,7 +339,7 @@ __global__ __launch_bounds__(kThreads, 2) void proj_kernel(Proj p) {
   }
 }
 
-template <bool WT, ProjEpilogue EPI>
+template <bool WT, ProjEpilogue EPI, int FMT = DCP_ACT_BF16>
 hipError_t launch(Proj p, hipStream_t s) {
   // Tiles of 128 tokens, unless they leave CUs without one.  Three outputs,
   // hidden 1,152, tiles of 128 / 64 tokens: 1,000 tokens (144 tiles of 128)
@@ -329,9 +351,9 @@ hipError_t launch(Proj p, hipStream_t s) {
   p.n_tiles = tiles(small ? 1 : 2);
   const dim3 grid((p.n_tiles + kNumXcd - 1) / kNumXcd * kNumXcd);
   if (small)
-    hipLaunchKernelGGL((proj_kernel<WT, 1, EPI>), grid, dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL((proj_kernel<WT, 1, EPI, FMT>), grid, dim3(kThreads), 0, s, p);
   else
-    hipLaunchKernelGGL((proj_kernel<WT, 2, EPI>), grid, dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL((proj_kernel<WT, 2, EPI, FMT>), grid, dim3(kThreads), 0, s, p);
   return hipGetLastError();
 }
 
@@ -345,6 +367,10 @@ hipError_t launch_proj(const Proj& p, ProjEpilogue epi, hipStream_t s) {
     case ProjEpilogue::kStoreT: return launch<true, ProjEpilogue::kStoreT>(p, s);
     case ProjEpilogue::kGelu: return launch<false, ProjEpilogue::kGelu>(p, s);
     case ProjEpilogue::kGeluGrad: return launch<true, ProjEpilogue::kGeluGrad>(p, s);
+    case ProjEpilogue::kGeluKeep:
+      return p.format == DCP_ACT_INT8 ? launch<false, ProjEpilogue::kGeluKeep, DCP_ACT_INT8>(p, s)
+                                      : launch<false, ProjEpilogue::kGeluKeep, DCP_ACT_E4M3>(p, s);
+    case ProjEpilogue::kGeluBack: return launch<true, ProjEpilogue::kGeluBack>(p, s);
     default: return launch<true, ProjEpilogue::kSumF32>(p, s);
   }
 }
