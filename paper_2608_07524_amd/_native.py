@@ -635,31 +635,37 @@ def _enqueue(torch, device, fn, *args):
         raise DCPError(st, last_error())
 
 
+def _require(torch, name, t, shape, dtype, device):
+    """A contiguous tensor of this shape, type (one, or a tuple of them) and device."""
+    if isinstance(t, torch.Tensor) and t.shape == shape and t.device == device and t.is_contiguous() \
+            and (t.dtype == dtype or (isinstance(dtype, tuple) and t.dtype in dtype)):
+        return
+    if not isinstance(t, torch.Tensor) or t.shape != shape:
+        raise ValueError(f"{name} must be a tensor of shape {tuple(shape)}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not {device}")
+    kinds = dtype if isinstance(dtype, tuple) else (dtype,)
+    raise ValueError(f"{name} must be contiguous and {' or '.join(str(k) for k in kinds)}")
+
+
+def _on_gpu(t):
+    if not t.is_cuda:
+        raise ValueError("tensors must be on a CUDA (HIP) device")
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
 def _act_dtype(torch, fmt: str):
     if fmt not in ("int8", "e4m3"):
-        raise ValueError(f"fmt must be 'int8' or 'e4m3', not {fmt!r}")
+        raise ValueError(f"the format must be 'int8' or 'e4m3', not {fmt!r}")
     return torch.int8 if fmt == "int8" else torch.float8_e4m3fn
 
 
-def _act_format(torch, codes) -> int:
-    fmt = {torch.int8: ACT_INT8, torch.float8_e4m3fn: ACT_E4M3, torch.bfloat16: ACT_BF16}.get(codes.dtype)
-    if fmt is None:
-        raise ValueError(f"codes must be int8 or float8_e4m3fn, not {codes.dtype}")
-    return fmt
-
-
-def _same_device(ref, name, others):
-    """Everything in ``others`` (name, tensor) is on ref's CUDA device."""
-    if not ref.is_cuda:
-        raise ValueError("tensors must be on a CUDA (HIP) device")
-    for n, t in others:
-        if t.device != ref.device:
-            raise ValueError(f"{n} is on {t.device}, {name} on {ref.device}")
-
-
-def _check_rows(torch, t, name, shape=None):
+def _rows(torch, name, t, shape=None):
     """A bf16 [rows, cols] matrix of contiguous rows; returns its row stride."""
-    if not hasattr(t, "dim") or t.dim() != 2 or t.dtype != torch.bfloat16:
+    if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.dtype != torch.bfloat16:
         raise ValueError(f"{name} must be a bf16 tensor of shape [rows, cols]")
     if shape is not None and t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
@@ -670,17 +676,19 @@ def _check_rows(torch, t, name, shape=None):
     return t.stride(0)
 
 
-def _check_codes(torch, codes, scales, shape=None):
-    """A checkpoint: contiguous codes [rows, cols] and their uint8 scale bytes."""
-    if not hasattr(codes, "dim") or codes.dim() != 2 or not codes.is_contiguous():
-        raise ValueError("codes must be a contiguous tensor of shape [rows, cols]")
+def _checkpoint(torch, name, codes, scales, shape=None, device=None):
+    """A checkpoint: contiguous codes [rows, cols] and their uint8 scale bytes; returns
+    its format."""
+    if not isinstance(codes, torch.Tensor) or codes.dim() != 2:
+        raise ValueError(f"{name}: codes must be a tensor of shape [rows, cols]")
+    fmt = ACT_INT8 if codes.dtype == torch.int8 else ACT_E4M3 if codes.dtype == torch.float8_e4m3fn else None
+    if fmt is None:
+        raise ValueError(f"{name}: codes must be int8 or float8_e4m3fn, not {codes.dtype}")
+    device = codes.device if device is None else device
+    _require(torch, name, codes, codes.shape if shape is None else shape, codes.dtype, device)
     rows, cols = codes.shape
-    if shape is not None and codes.shape != shape:
-        raise ValueError(f"codes have shape {tuple(codes.shape)}, not {tuple(shape)}")
-    want = (rows, -(-cols // ACT_GROUP))
-    if not hasattr(scales, "dim") or scales.shape != want or scales.dtype != torch.uint8 \
-            or not scales.is_contiguous():
-        raise ValueError(f"scales must be a contiguous uint8 tensor of shape {want}")
+    _require(torch, name + "'s scales", scales, (rows, -(-cols // ACT_GROUP)), torch.uint8, device)
+    return fmt
 
 
 def act8_pack(x, fmt: str = "int8", codes=None, scales=None):
@@ -690,16 +698,15 @@ def act8_pack(x, fmt: str = "int8", codes=None, scales=None):
     a multiple of 8)."""
     import torch
     dtype = _act_dtype(torch, fmt)
-    ld = _check_rows(torch, x, "x")
+    ld = _rows(torch, "x", x)
     rows, cols = x.shape
-    _same_device(x, "x", [(n, t) for n, t in (("codes", codes), ("scales", scales)) if t is not None])
-    given = codes is not None or scales is not None
-    codes = x.new_empty((rows, cols), dtype=dtype) if codes is None else codes
+    if codes is not None:
+        _require(torch, "codes", codes, x.shape, dtype, x.device)
+    if scales is not None:
+        _require(torch, "scales", scales, (rows, -(-cols // ACT_GROUP)), torch.uint8, x.device)
+    _on_gpu(x)
+    codes = torch.empty_like(x, dtype=dtype, memory_format=torch.contiguous_format) if codes is None else codes
     scales = x.new_empty((rows, -(-cols // ACT_GROUP)), dtype=torch.uint8) if scales is None else scales
-    if given:
-        _check_codes(torch, codes, scales, x.shape)
-        if codes.dtype != dtype:
-            raise ValueError(f"codes must be {dtype} for fmt {fmt!r}")
     d = Act8DescC(rows, cols, ACT_FORMATS[fmt], ld)
     _enqueue(torch, x.device, load().dcp_act8_pack, d, x.data_ptr(), codes.data_ptr(), scales.data_ptr())
     return codes, scales
@@ -708,16 +715,15 @@ def act8_pack(x, fmt: str = "int8", codes=None, scales=None):
 def act8_unpack(codes, scales, out=None):
     """The bf16 values of an 8-bit checkpoint (see dcp_act8_unpack)."""
     import torch
-    _check_codes(torch, codes, scales)
-    fmt = _act_format(torch, codes)
-    if fmt == ACT_BF16:
-        raise ValueError("codes must be int8 or float8_e4m3fn")
-    _same_device(codes, "codes", [("scales", scales)] + ([("out", out)] if out is not None else []))
+    fmt = _checkpoint(torch, "codes", codes, scales)
     rows, cols = codes.shape
-    if out is None:
-        out, ld = torch.empty_like(codes, dtype=torch.bfloat16), cols
-    else:
-        ld = _check_rows(torch, out, "out", codes.shape)
+    ld = cols
+    if out is not None:
+        ld = _rows(torch, "out", out, codes.shape)
+        if out.device != codes.device:
+            raise ValueError(f"out is on {out.device}, codes on {codes.device}")
+    _on_gpu(codes)
+    out = torch.empty_like(codes, dtype=torch.bfloat16) if out is None else out
     d = Act8DescC(rows, cols, fmt, ld)
     _enqueue(torch, codes.device, load().dcp_act8_unpack, d, codes.data_ptr(), scales.data_ptr(), out.data_ptr())
     return out
@@ -729,23 +735,22 @@ def act8_gelu_bwd(codes, scales, da, du=None, a=None):
     ``scales`` None."""
     import torch
     if scales is None:
-        if not hasattr(codes, "dim") or codes.dtype != torch.bfloat16 or codes.dim() != 2 or not codes.is_contiguous():
-            raise ValueError("without scales u must be a contiguous bf16 tensor of shape [rows, cols]")
+        fmt = ACT_BF16
+        if not isinstance(codes, torch.Tensor) or codes.dim() != 2:
+            raise ValueError("u must be a tensor of shape [rows, cols]")
+        _require(torch, "u (without scales)", codes, codes.shape, torch.bfloat16, codes.device)
     else:
-        _check_codes(torch, codes, scales)
-    fmt = _act_format(torch, codes)
-    if (fmt == ACT_BF16) != (scales is None):
-        raise ValueError("scales go with int8 or float8_e4m3fn codes")
-    given = [(n, t) for n, t in (("scales", scales), ("da", da), ("du", du), ("a", a)) if t is not None]
-    for n, t in given[1 if scales is not None else 0:]:
-        _check_matrix(torch, n, t, codes.shape)
-    _same_device(codes, "codes", given)
+        fmt = _checkpoint(torch, "codes", codes, scales)
+    for name, t in (("da", da), ("du", du), ("a", a)):
+        if t is not None or name == "da":
+            _require(torch, name, t, codes.shape, torch.bfloat16, codes.device)
+    _on_gpu(codes)
     du = torch.empty_like(da) if du is None else du
     a = torch.empty_like(da) if a is None else a
     rows, cols = codes.shape
     d = Act8DescC(rows, cols, fmt, cols)
-    _enqueue(torch, da.device, load().dcp_act8_gelu_bwd, d, codes.data_ptr(), None if scales is None else
-             scales.data_ptr(), da.data_ptr(), du.data_ptr(), a.data_ptr())
+    _enqueue(torch, da.device, load().dcp_act8_gelu_bwd, d, codes.data_ptr(), _ptr(scales), da.data_ptr(),
+             du.data_ptr(), a.data_ptr())
     return du, a
 
 
@@ -774,20 +779,14 @@ class GatedNormGrads(NamedTuple):
     dpre: object
 
 
-def _ptr(t):
-    return None if t is None else t.data_ptr()
-
-
 def _join_weights(torch, shape, post, gate, pre, cu_seqlens, device):
     """Checks the weights of a join over [rows, hidden]; returns (n_seqs, the
     device tensor of offsets or None)."""
     rows, h = shape
-    on = []
-    for name, t in (("post", post), ("pre", pre)):
-        if t is not None:
-            if t.shape != (h,) or t.dtype != torch.bfloat16 or not t.is_contiguous():
-                raise ValueError(f"{name} must be a contiguous bf16 tensor of shape ({h},)")
-            on.append((name, t))
+    if post is not None:
+        _require(torch, "post", post, (h,), torch.bfloat16, device)
+    if pre is not None:
+        _require(torch, "pre", pre, (h,), torch.bfloat16, device)
     n = 0
     if cu_seqlens is not None:
         if gate is None:
@@ -797,27 +796,15 @@ def _join_weights(torch, shape, post, gate, pre, cu_seqlens, device):
             if cu[0] != 0 or np.any(np.diff(cu) < 0) or int(cu[-1]) > rows:
                 raise ValueError("cu_seqlens must start at 0, not decrease and end within the rows")
             cu_seqlens = torch.from_numpy(cu).to(device)
-        elif cu_seqlens.dim() != 1 or cu_seqlens.dtype != torch.int32 or not cu_seqlens.is_contiguous() \
-                or cu_seqlens.numel() < 2:
-            raise ValueError("cu_seqlens on a device must be a contiguous int32 tensor of at least two offsets")
+        elif cu_seqlens.dim() != 1 or cu_seqlens.numel() < 2:
+            raise ValueError("cu_seqlens on a device must hold at least two offsets")
+        else:
+            _require(torch, "cu_seqlens", cu_seqlens, cu_seqlens.shape, torch.int32, device)
         n = cu_seqlens.numel() - 1
-        on.append(("cu_seqlens", cu_seqlens))
     if gate is not None:
-        want = [(n, h)] if n else [(h,), (1, h)]
-        if gate.shape not in want or gate.dtype != torch.bfloat16 or not gate.is_contiguous():
-            raise ValueError(f"gate must be a contiguous bf16 tensor of shape {want[0]}")
-        on.append(("gate", gate))
-    for name, t in on:
-        if t.device != device:
-            raise ValueError(f"{name} is on {t.device}, the activations on {device}")
+        one = n == 0 and isinstance(gate, torch.Tensor) and gate.dim() == 2
+        _require(torch, "gate", gate, (n, h) if n else (1, h) if one else (h,), torch.bfloat16, device)
     return n, cu_seqlens
-
-
-def _check_matrix(torch, name, t, shape, dtypes=None):
-    if not hasattr(t, "dim") or t.shape != shape:
-        raise ValueError(f"{name} must be a tensor of shape {tuple(shape)}")
-    if t.dtype not in (dtypes or (torch.bfloat16,)) or not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous and bf16" + (" or float32" if dtypes else ""))
 
 
 def gated_norm_fwd(x, f, post=None, gate=None, pre=None, cu_seqlens=None, residual_scale: float = 1.0,
@@ -830,21 +817,24 @@ def gated_norm_fwd(x, f, post=None, gate=None, pre=None, cu_seqlens=None, residu
     ``y`` are left as they are.  ``keep_f`` / ``keep_out`` ("int8" or "e4m3", one
     format a call) also return the checkpoint of f / of out."""
     import torch
-    if not hasattr(x, "dim") or x.dim() != 2:
+    if not isinstance(x, torch.Tensor) or x.dim() != 2:
         raise ValueError("x must be a tensor of shape [rows, hidden]")
-    given = [("x", x), ("f", f)] + [(n, t) for n, t in (("out", out), ("y", y)) if t is not None]
-    for n, t in given:
-        _check_matrix(torch, n, t, x.shape)
-    if y is not None and pre is None:
-        raise ValueError("y needs the gain pre")
-    kinds = {k for k in (keep_f, keep_out) if k is not None}
-    if len(kinds) > 1:
+    shape, dev, bf16 = x.shape, x.device, torch.bfloat16
+    _require(torch, "x", x, shape, bf16, dev)
+    _require(torch, "f", f, shape, bf16, dev)
+    if out is not None:
+        _require(torch, "out", out, shape, bf16, dev)
+    if y is not None:
+        _require(torch, "y", y, shape, bf16, dev)
+        if pre is None:
+            raise ValueError("y needs the gain pre")
+    if keep_f is not None and keep_out is not None and keep_f != keep_out:
         raise ValueError("keep_f and keep_out must be one format")
-    fmt = kinds.pop() if kinds else "bf16"
-    dtype = None if fmt == "bf16" and keep_f is None and keep_out is None else _act_dtype(torch, fmt)
-    _same_device(x, "x", given[1:])
-    n, cu = _join_weights(torch, x.shape, post, gate, pre, cu_seqlens, x.device)
-    rows, h = x.shape
+    fmt = keep_f or keep_out
+    dtype = None if fmt is None else _act_dtype(torch, fmt)
+    n, cu = _join_weights(torch, shape, post, gate, pre, cu_seqlens, dev)
+    _on_gpu(x)
+    rows, h = shape
     out = torch.empty_like(x) if out is None else out
     if pre is not None and y is None:
         y = torch.empty_like(x)
@@ -854,15 +844,24 @@ def gated_norm_fwd(x, f, post=None, gate=None, pre=None, cu_seqlens=None, residu
     def kept(on):
         if on is None:
             return None, None
-        t = (x.new_empty((rows, h), dtype=dtype), x.new_empty((rows, -(-h // ACT_GROUP)), dtype=torch.uint8))
+        t = torch.empty_like(x, dtype=dtype), x.new_empty((rows, -(-h // ACT_GROUP)), dtype=torch.uint8)
         return t, KeptC(t[0].data_ptr(), t[1].data_ptr())
 
     (f8, kf), (out8, ko) = kept(keep_f), kept(keep_out)
-    d = GatedNormDescC(rows, h, n, _ptr(cu), float(residual_scale), float(eps), ACT_FORMATS[fmt], 0, 0)
+    d = GatedNormDescC(rows, h, n, _ptr(cu), residual_scale, eps, ACT_FORMATS[fmt or "bf16"], 0, 0)
     w = GatedNormPtrsC(_ptr(post), _ptr(gate), _ptr(pre))
-    _enqueue(torch, x.device, load().dcp_gated_norm_fwd, d, w, x.data_ptr(), f.data_ptr(), out.data_ptr(), _ptr(y),
+    _enqueue(torch, dev, load().dcp_gated_norm_fwd, d, w, x.data_ptr(), f.data_ptr(), out.data_ptr(), _ptr(y),
              _ptr(rstd_f), _ptr(rstd_out), kf, ko)
     return GatedNorm(out, y, rstd_f, rstd_out, f8, out8)
+
+
+def _kept(torch, name, t, shape, device):
+    """An activation kept in bf16, or its checkpoint (codes, scales): (format, its C form)."""
+    if isinstance(t, (tuple, list)) and len(t) == 2:
+        fmt = _checkpoint(torch, name, t[0], t[1], shape, device)
+        return fmt, KeptC(t[0].data_ptr(), t[1].data_ptr())
+    _require(torch, name, t, shape, torch.bfloat16, device)
+    return ACT_BF16, KeptC(t.data_ptr(), None)
 
 
 def gated_norm_bwd(dout, dy=None, f=None, out=None, rstd_f=None, rstd_out=None, post=None, gate=None, pre=None,
@@ -875,76 +874,53 @@ def gated_norm_bwd(dout, dy=None, f=None, out=None, rstd_f=None, rstd_out=None, 
     sequence are left as they are."""
     import torch
     ref = dout if dout is not None else dy
-    if not hasattr(ref, "dim") or ref.dim() != 2:
+    if not isinstance(ref, torch.Tensor) or ref.dim() != 2:
         raise ValueError("dout (or, without it, dy) must be a tensor of shape [rows, hidden]")
-    if pre is None and (dy is not None or want_y or y is not None):
-        raise ValueError("dy and y need the gain pre")
-    if pre is not None and dy is None:
-        raise ValueError("the gain pre needs dy")
-    shape = ref.shape
+    shape, dev, bf16, f32 = ref.shape, ref.device, torch.bfloat16, torch.float32
     rows, h = shape
-    on = []
-    for n_, t in (("dout", dout), ("dx", dx), ("df", df), ("y", y)):
+    if dout is not None:
+        _require(torch, "dout", dout, shape, bf16, dev)
+    for name, t in (("dx", dx), ("df", df), ("y", y)):
         if t is not None:
-            _check_matrix(torch, n_, t, shape)
-            on.append((n_, t))
-    if dy is not None:
-        _check_matrix(torch, "dy", dy, shape, (torch.bfloat16, torch.float32))
-        on.append(("dy", dy))
-    fmts = set()
-
-    def kept(name, t, needed):
-        if not needed:
-            return None
-        if t is None:
-            raise ValueError(f"{name} is needed for these weights")
-        if isinstance(t, (tuple, list)):
-            codes, scales = t
-            _check_codes(torch, codes, scales, shape)
-            fmt = _act_format(torch, codes)
-            if fmt == ACT_BF16:
-                raise ValueError(f"{name}: codes must be int8 or float8_e4m3fn")
-            fmts.add(fmt)
-            on.extend([(name, codes), (name + "'s scales", scales)])
-            return KeptC(codes.data_ptr(), scales.data_ptr())
-        _check_matrix(torch, name, t, shape)
-        fmts.add(ACT_BF16)
-        on.append((name, t))
-        return KeptC(t.data_ptr(), None)
-
-    kf = kept("f", f, post is not None or gate is not None)
-    ko = kept("out", out, pre is not None)
-    if len(fmts) > 1:
+            _require(torch, name, t, shape, bf16, dev)
+    kf = ko = None
+    kinds = set()
+    if post is not None or gate is not None:
+        kind, kf = _kept(torch, "f", f, shape, dev)
+        kinds.add(kind)
+    if post is not None:
+        _require(torch, "rstd_f", rstd_f, (rows,), f32, dev)
+    if pre is not None:
+        _require(torch, "dy", dy, shape, (bf16, f32), dev)
+        kind, ko = _kept(torch, "out", out, shape, dev)
+        kinds.add(kind)
+        _require(torch, "rstd_out", rstd_out, (rows,), f32, dev)
+    elif dy is not None or want_y or y is not None:
+        raise ValueError("dy and y need the gain pre")
+    if len(kinds) > 1:
         raise ValueError("f and out must be kept in one format")
-    for n_, t, needed in (("rstd_f", rstd_f, post is not None), ("rstd_out", rstd_out, pre is not None)):
-        if needed:
-            if not hasattr(t, "dim") or t.shape != (rows,) or t.dtype != torch.float32 or not t.is_contiguous():
-                raise ValueError(f"{n_} must be a contiguous float32 tensor of shape ({rows},)")
-            on.append((n_, t))
-    if workspace is not None:
-        if not workspace.is_contiguous():
-            raise ValueError("workspace must be contiguous")
-        on.append(("workspace", workspace))
-    _same_device(ref, "dout", on)
-    n, cu = _join_weights(torch, shape, post, gate, pre, cu_seqlens, ref.device)
+    n, cu = _join_weights(torch, shape, post, gate, pre, cu_seqlens, dev)
+    if workspace is not None and (workspace.device != dev or not workspace.is_contiguous()):
+        raise ValueError(f"workspace must be contiguous and on {dev}")
+    _on_gpu(ref)
     lib = load()
-    d = GatedNormDescC(rows, h, n, _ptr(cu), float(residual_scale), 0.0, fmts.pop() if fmts else ACT_BF16,
-                       int(dy is not None and dy.dtype == torch.float32), 0)
-    w = GatedNormPtrsC(_ptr(post), _ptr(gate), _ptr(pre))
+    d = GatedNormDescC(rows, h, n, _ptr(cu), residual_scale, 0.0, kinds.pop() if kinds else ACT_BF16,
+                       int(dy is not None and dy.dtype == f32), 0)
     size = C.c_size_t()
-    _check(lib.dcp_gated_norm_bwd_workspace_size(d, C.byref(size)))
-    empty = lambda: torch.empty_like(ref, dtype=torch.bfloat16)
+    _check(lib.dcp_gated_norm_bwd_workspace_size(d, size))
     if want_dx and dx is None:
-        dx = empty()
-    df = empty() if df is None else df
+        dx = torch.empty_like(ref, dtype=bf16)
+    df = torch.empty_like(ref, dtype=bf16) if df is None else df
     if want_y and y is None:
-        y = empty()
-    dpost, dgate, dpre = (None if t is None else torch.empty_like(t, dtype=torch.float32) for t in (post, gate, pre))
+        y = torch.empty_like(ref, dtype=bf16)
+    dpost = None if post is None else torch.empty_like(post, dtype=f32)
+    dgate = None if gate is None else torch.empty_like(gate, dtype=f32)
+    dpre = None if pre is None else torch.empty_like(pre, dtype=f32)
     if workspace is None:
         workspace = ref.new_empty((size.value,), dtype=torch.uint8)
-    _enqueue(torch, ref.device, lib.dcp_gated_norm_bwd, d, w, _ptr(dout), _ptr(dy), kf, ko, _ptr(rstd_f),
-             _ptr(rstd_out), _ptr(dx), df.data_ptr(), _ptr(y), GatedNormPtrsC(_ptr(dpost), _ptr(dgate), _ptr(dpre)),
-             workspace.data_ptr(), _nbytes(workspace))
+    _enqueue(torch, dev, lib.dcp_gated_norm_bwd, d, GatedNormPtrsC(_ptr(post), _ptr(gate), _ptr(pre)), _ptr(dout),
+             _ptr(dy), kf, ko, _ptr(rstd_f), _ptr(rstd_out), _ptr(dx), df.data_ptr(), _ptr(y),
+             GatedNormPtrsC(_ptr(dpost), _ptr(dgate), _ptr(dpre)), workspace.data_ptr(), _nbytes(workspace))
     return GatedNormGrads(dx, df, y, dpost, dgate, dpre)
 
 
@@ -999,8 +975,7 @@ class Block:
                 if not ok or t.dtype != dtype or not t.is_contiguous() or t.device != dev:
                     raise ValueError(f"{what}[{name!r}] must be a contiguous {dtype} tensor of shape {want[name]} "
                                      f"on {dev}")
-        if not dev.type == "cuda":
-            raise ValueError("tensors must be on a CUDA (HIP) device")
+        _on_gpu(weights["wq"])
         self.weights, self.grads = weights, grads
         self.scale = 1.0 / math.sqrt(head_dim) if scale is None else scale
         self.d = _Desc(cu, T, n_heads, head_dim, self.scale, causal)
@@ -1028,9 +1003,7 @@ class Block:
         self.stash = None
 
     def _matrix(self, name, t):
-        _check_matrix(self.torch, name, t, (self.T, self.hidden))
-        if t.device != self.ws.device:
-            raise ValueError(f"{name} is on {t.device}, the block on {self.ws.device}")
+        _require(self.torch, name, t, (self.T, self.hidden), self.torch.bfloat16, self.ws.device)
 
     def fwd(self, x, keep: bool = True, out=None, stash=None):
         """``stash``: a preallocated uint8 buffer of stash_bytes to keep into."""
