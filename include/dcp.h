@@ -16,6 +16,11 @@
  *                        (DCP-intra, Sec. 3.4 / Algorithm 1; DCP-inter,
  *                        Sec. 3.3 / Eq. (3) / Appendix C).
  *
+ * and what surrounds them in a model: the transformer layer that the profile
+ * times (dcp_layer_*), 8-bit activation checkpoints that make its stash smaller
+ * (dcp_act8_*), the gated, normed join of a branch into the residual stream
+ * (dcp_gated_norm_*), and the block made of all three (dcp_block_*).
+ *
  * Conventions shared by every call
  * --------------------------------
  * - Status: every call returns 0 (DCP_OK) or a negative dcp_status and never
@@ -589,8 +594,8 @@ typedef struct {
  *   dx    may be NULL (residual_scale 1 and no pre: it would equal dout).
  *   y     may be NULL; needs pre.
  * A gate's gradient is summed over its sequence's rows (0 for an empty one), or
- * over all rows where one gate serves all.  Sums are fp32, in an order fixed by rows
- * and hidden: results are bitwise reproducible.  dx or df may be dout's buffer, y, dx
+ * over all rows where one gate serves all.  Sums are fp32, in an order fixed by rows,
+ * hidden and the offsets: results are bitwise reproducible.  dx or df may be dout's buffer, y, dx
  * or df a bf16 dy's.  The three gradients are distinct buffers.  Two calls that
  * overlap in time need two workspaces.
  */

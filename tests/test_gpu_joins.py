@@ -166,6 +166,43 @@ def test_checkpoints_of_more_than_2_31_elements(torch, P):
         assert torch.equal(P.act8_unpack(c, b), back[lo:lo + 300])
 
 
+def test_checkpoints_of_more_than_2_31_pieces(torch, P):
+    """More 8-column pieces than one launch counts: the rest is a second one."""
+    rows, cols = 131_080, 131_072  # 2^31 + 131,072 pieces; 34 GB, read back in place
+    x = torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda")
+    x[:9].normal_()
+    x[9:-18] = 1.0
+    x[-18:] = x[:9].repeat(2, 1)
+    want = x[:9].clone()
+    codes, s = P.act8_pack(x)
+    P.act8_unpack(codes, s, out=x)
+    c, b = P.act8_pack(want)
+    held = P.act8_unpack(c, b)
+    for lo in (0, rows - 18, rows - 9):
+        assert torch.equal(codes[lo:lo + 9], c) and torch.equal(s[lo:lo + 9], b) and torch.equal(x[lo:lo + 9], held)
+    assert bool((x[65_000:65_010] == 1.0).all())
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "int8", "e4m3"])
+def test_gelu_backward_in_wider_matrices(torch, P, fmt):
+    """The C call on slices: row strides of da, du, a (and a bf16 u) beyond cols."""
+    from paper_2608_07524_amd import _native as N
+    rows, cols, ld = 37, 72, 200
+    rng = np.random.default_rng(11)
+    u, da = (to_device(torch, _bits(rng.standard_normal((rows, cols)))) for _ in range(2))
+    wide = lambda: torch.full((rows, ld), 7.0, dtype=torch.bfloat16, device="cuda")
+    uw, dw, o1, o2 = wide(), wide(), wide(), wide()
+    uw[:, :cols], dw[:, :cols] = u, da
+    kept = (u, None) if fmt == "bf16" else P.act8_pack(u, fmt)
+    want = P.act8_gelu_bwd(*kept, da)
+    d = N.Act8DescC(rows, cols, N.ACT_FORMATS[fmt], ld)
+    src = (uw.data_ptr(), None) if fmt == "bf16" else tuple(t.data_ptr() for t in kept)
+    N._check(N.load().dcp_act8_gelu_bwd(d, *src, dw.data_ptr(), o1.data_ptr(), o2.data_ptr(),
+                                        torch.cuda.current_stream().cuda_stream))
+    for got, ref in zip((o1, o2), want):
+        assert torch.equal(got[:, :cols], ref) and bool((got[:, cols:] == 7.0).all())
+
+
 def test_no_rows(torch, P):
     x = torch.empty(0, 64, dtype=torch.bfloat16, device="cuda")
     codes, s = P.act8_pack(x)
@@ -328,6 +365,12 @@ def test_join_in_place_and_repeatable(torch, P):
     z = back(dout=torch.zeros_like(dout))
     y = P.gated_norm_bwd(None, dy, f, a.out, a.rstd_f, a.rstd_out, cu_seqlens=cu, want_dx=False, **wt)
     assert torch.equal(z.df, y.df) and y.dx is None and torch.equal(z.dpre, y.dpre)
+    f32 = P.gated_norm_bwd(None, dy.float(), f, a.out, a.rstd_f, a.rstd_out, cu_seqlens=cu, **wt)
+    assert torch.equal(z.df, f32.df) and torch.equal(z.dx, f32.dx)
+    ws = torch.full((1 << 24,), 255, dtype=torch.uint8, device="cuda")  # (a workspace need not be cleared)
+    own = back(workspace=ws)
+    for n in ("dx", "df", "y", "dpost", "dgate", "dpre"):
+        assert torch.equal(getattr(p, n), getattr(own, n)), n
 
 
 def test_join_host_offsets_and_one_gate_row(torch, P):
