@@ -21,6 +21,7 @@
 
 #include "act8.h"
 #include "block_launch.h"
+#include "tile_shapes.h"
 
 namespace dcp {
 namespace {
@@ -39,7 +40,15 @@ struct Team {
   static constexpr int kBlock = TL > 128 ? TL : 256, kTeams = kBlock / TL;
   static constexpr int kSub = TL < 64 ? TL : 64;       // lanes of a team within a wavefront
   static constexpr int kWaves = TL < 64 ? 1 : TL / 64;  // wavefronts a team spans
+  // What all lanes of a team have alike is in scalar registers where a wavefront has one team.
+  static __device__ __forceinline__ int alike(int v) { return TL < 64 ? v : __builtin_amdgcn_readfirstlane(v); }
 };
+typedef uint32_t row_t;  // rows < 2^31, and at most a workgroup's more
+__device__ __forceinline__ row_t offset_of(const int32_t* cu, int s) { return row_t(max(cu[s], 0)); }
+// Rows in use: all, or those of the sequences.
+__device__ __forceinline__ row_t rows_of(int64_t rows, const int32_t* cu, int n_seqs) {
+  return cu ? min(row_t(rows), offset_of(cu, n_seqs)) : row_t(rows);
+}
 
 // Sums of N values over a team.  Teams of several wavefronts meet once, in the half
 // of `red` that belongs to this row's parity: the other half's readers are at most
@@ -72,13 +81,13 @@ __device__ __forceinline__ void team_total(float (&v)[N], float* red, int parity
 // wavefront (64: three steps reach 2^18 sequences).  Whatever cu holds, s stays in
 // [0, n].
 template <int L>
-__device__ __forceinline__ int sequence_of(const int32_t* cu, int n, int64_t row) {
+__device__ __forceinline__ int sequence_of(const int32_t* cu, int n, row_t row) {
   const int lane = threadIdx.x & (L - 1), shift = threadIdx.x & 63 & ~(L - 1);
   const uint64_t mask = L == 64 ? ~uint64_t(0) : (uint64_t(1) << (L & 63)) - 1;
   int lo = 0, len = n + 1;
   while (len > 1) {
     const int step = (len + L - 1) / L, at = lane * step;
-    const bool below = at < len && int64_t(cu[lo + at]) <= row;
+    const bool below = at < len && offset_of(cu, lo + at) <= row;
     const int c = max(int(__popcll((__ballot(below) >> shift) & mask)) - 1, 0);
     lo += c * step;
     len = min(step, len - c * step);
@@ -86,41 +95,58 @@ __device__ __forceinline__ int sequence_of(const int32_t* cu, int n, int64_t row
   return lo;
 }
 
-// Follows a team's consecutive rows through cu_seqlens.
+// Follows a team's consecutive rows through cu_seqlens, one offset ahead of them.
+template <int TL>
 struct Walk {
-  const int32_t* cu;
-  int n, s;
-  int64_t end;  // first row behind sequence s
-  template <int L>
-  __device__ __forceinline__ void start(const int32_t* c, int n_seqs, int64_t row) {
+  const int32_t* cu = nullptr;
+  int n = 0, s = 0;
+  row_t begin = 0, end = ~row_t(0), end2 = 0;  // rows of sequence s, and the end of the next one
+  __device__ __forceinline__ row_t at(int i) const { return row_t(Team<TL>::alike(int(offset_of(cu, i)))); }
+  __device__ __forceinline__ void start(const int32_t* c, int n_seqs, row_t row) {
     cu = c;
     n = n_seqs;
-    s = min(sequence_of<L>(c, n_seqs, row), n_seqs - 1);
-    end = cu[s + 1];
+    s = Team<TL>::alike(min(sequence_of<Team<TL>::kSub>(c, n_seqs, row), n_seqs - 1));
+    begin = at(s);
+    end = at(s + 1);
+    end2 = at(min(s + 2, n));
   }
-  // to the sequence of `row`, if that is a later one
-  __device__ __forceinline__ void step(int64_t row) {
-    while (row >= end && s < n - 1) end = cu[++s + 1];
+  // To the sequence of `row`, which lies behind sequence s; returns how many further.
+  __device__ __forceinline__ int step(row_t row) {
+    const int from = s;
+    while (row >= end && s < n - 1) {
+      ++s;
+      begin = end;
+      end = end2;
+      end2 = at(min(s + 2, n));
+    }
+    return s - from;
   }
 };
 
-// 8 values of a bf16 row at column c as fp32, 1 where there is none.
-__device__ __forceinline__ void gains(const __bf16* g, int c, int h, float (&v)[8]) {
-  if (g && c < h) {
-    const bf16x8 b = *reinterpret_cast<const bf16x8*>(g + c);
+// 8 values of a bf16 row at column c, 1 where there is none.
+__device__ __forceinline__ bf16x8 gain8(const __bf16* g, int c, int h) {
+  if (g && c < h) return *reinterpret_cast<const bf16x8*>(g + c);
+  bf16x8 one;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = float(b[e]);
-  } else {
+  for (int e = 0; e < 8; ++e) one[e] = __bf16(1.f);
+  return one;
+}
+// Keeps 8 values as they are, in bf16: without it the compiler converts what a loop does
+// not change before the loop and holds twice the registers through it.
+__device__ __forceinline__ void stay_packed(bf16x8& v) {
+  u32x4 w = __builtin_bit_cast(u32x4, v);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = 1.f;
+  for (int i = 0; i < 4; ++i) {
+    uint32_t x = w[i];
+    asm("" : "+v"(x));
+    w[i] = x;
   }
+  v = __builtin_bit_cast(bf16x8, w);
 }
 __device__ __forceinline__ void gains_product(const __bf16* a, const __bf16* b, int c, int h, float (&v)[8]) {
-  float w[8];
-  gains(a, c, h, v);
-  gains(b, c, h, w);
+  const bf16x8 x = gain8(a, c, h), y = gain8(b, c, h);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] *= w[e];
+  for (int e = 0; e < 8; ++e) v[e] = float(x[e]) * float(y[e]);
 }
 __device__ __forceinline__ bf16x8 rounded(const float (&v)[8]) {
   bf16x8 b;
@@ -130,10 +156,10 @@ __device__ __forceinline__ bf16x8 rounded(const float (&v)[8]) {
 }
 
 template <int FMT>
-__device__ __forceinline__ void keep8(void* codes, void* scales, bf16x8 v, int64_t row, int c, int h, int groups) {
+__device__ __forceinline__ void keep8(void* codes, void* scales, bf16x8 v, row_t row, int c, int h, int groups) {
   const uint32_t byte = scale_byte<FMT>(group_top(top_bits(v)));
-  if (c < h) *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(codes) + row * h + c) = encode8<FMT>(v, byte);
-  if (c < h && (c & 31) == 0) static_cast<uint8_t*>(scales)[row * groups + (c >> 5)] = uint8_t(byte);
+  if (c < h) *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(codes) + int64_t(row) * h + c) = encode8<FMT>(v, byte);
+  if (c < h && (c & 31) == 0) static_cast<uint8_t*>(scales)[int64_t(row) * groups + (c >> 5)] = uint8_t(byte);
 }
 
 // KEEP: format of the checkpoints (DCP_ACT_BF16: none).  y and its statistics come
@@ -144,33 +170,29 @@ __global__ __launch_bounds__(Team<TL>::kBlock) void gated_norm_fwd_kernel(GatedN
   __shared__ float red[2][2][T::kBlock / 64];
   const int lane = threadIdx.x % TL, c = 8 * lane, h = p.hidden, groups = (h + kActGroup - 1) / kActGroup;
   const bool mine = c < h;
-  const int64_t block_first = int64_t(blockIdx.x) * T::kTeams * team_rows;
-  const int64_t first = block_first + int64_t(threadIdx.x / TL) * team_rows;
-  int64_t rows = p.rows;
-  if (p.cu) rows = min(rows, int64_t(p.cu[p.n_seqs]));
+  const row_t rows = rows_of(p.rows, p.cu, p.n_seqs), block_first = blockIdx.x * row_t(T::kTeams * team_rows);
+  const row_t first = block_first + row_t(T::alike(threadIdx.x / TL) * team_rows);
   if (block_first >= rows) return;
   // (teams that meet at barriers all take the first team's turns)
-  const int64_t left = rows - (T::kWaves > 1 ? block_first : first);
-  const int turns = int(min(left, int64_t(team_rows)));
+  const row_t lead = T::kWaves > 1 ? block_first : first;
+  const int turns = lead < rows ? int(min(rows - lead, row_t(team_rows))) : 0;
   const __bf16 *x = static_cast<const __bf16*>(p.x), *f = static_cast<const __bf16*>(p.f);
   const __bf16 *post = static_cast<const __bf16*>(p.post), *gate = static_cast<const __bf16*>(p.gate);
   bf16x8 xn{}, fn{};
-  auto fetch = [&](int64_t row) {
+  auto fetch = [&](row_t row) {
     if (mine && row < rows) {
-      fn = *reinterpret_cast<const bf16x8*>(f + row * h + c);
-      xn = *reinterpret_cast<const bf16x8*>(x + row * h + c);
+      fn = *reinterpret_cast<const bf16x8*>(f + int64_t(row) * h + c);
+      xn = *reinterpret_cast<const bf16x8*>(x + int64_t(row) * h + c);
     }
   };
   fetch(first);
-  float branch[8], pre[8];  // post o gate, pre
-  gains(static_cast<const __bf16*>(p.pre), c, h, pre);
-  Walk walk;
-  walk.s = 0;
-  walk.end = INT64_MAX;
-  if (p.cu && first < rows) walk.start<T::kSub>(p.cu, p.n_seqs, first);
+  float branch[8];  // post o gate
+  const bf16x8 pre8 = gain8(static_cast<const __bf16*>(p.pre), c, h);
+  Walk<TL> walk;
+  if (p.cu && first < rows) walk.start(p.cu, p.n_seqs, first);
   gains_product(post, gate ? gate + int64_t(walk.s) * h : nullptr, c, h, branch);
   for (int i = 0; i < turns; ++i) {
-    const int64_t row = first + i;
+    const row_t row = first + row_t(i);
     const bool live = row < rows;
     if (live && row >= walk.end) {
       walk.step(row);
@@ -197,7 +219,7 @@ __global__ __launch_bounds__(Team<TL>::kBlock) void gated_norm_fwd_kernel(GatedN
       r[0] += o[e] * o[e];
     }
     const bf16x8 ov = rounded(o);
-    if (live && mine) *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.out) + row * h + c) = ov;
+    if (live && mine) *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.out) + int64_t(row) * h + c) = ov;
     if constexpr (KEEP != DCP_ACT_BF16) {
       if (live && p.keep_f) keep8<KEEP>(p.keep_f, p.keep_f_scales, fv, row, c, h, groups);
       if (live && p.keep_out) keep8<KEEP>(p.keep_out, p.keep_out_scales, ov, row, c, h, groups);
@@ -207,8 +229,8 @@ __global__ __launch_bounds__(Team<TL>::kBlock) void gated_norm_fwd_kernel(GatedN
       const float ro = rsqrtf(r[0] / float(h) + p.eps);
       if (live && lane == 0) p.rstd_out[row] = ro;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] *= ro * pre[e];
-      if (live && mine) *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.y) + row * h + c) = rounded(o);
+      for (int e = 0; e < 8; ++e) o[e] *= ro * float(pre8[e]);
+      if (live && mine) *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.y) + int64_t(row) * h + c) = rounded(o);
     }
   }
 }
@@ -235,21 +257,29 @@ inline int team_lanes(int hidden) {
   while (l < need) l *= 2;
   return l;
 }
-constexpr int kBwdRowsMax = 32, kBwdBlocks = 768;
-inline BwdShape bwd_shape(int64_t rows, int hidden) {
+// Wavefronts that share a SIMD: 128 registers each where a team's rows and offsets are in
+// scalar registers, more otherwise.
+constexpr int bwd_waves(int lanes) { return lanes < 64 ? 3 : 4; }
+constexpr int kBwdRowsMax = 128, kShortRows = 64;
+inline BwdShape bwd_shape(int64_t rows, int hidden, int n_seqs) {
   BwdShape s;
   s.lanes = team_lanes(hidden);
   s.block = s.lanes > 128 ? s.lanes : 256;
   s.teams_of_block = s.block / s.lanes;
-  // Rows of a team: at most so many that there are kBwdBlocks workgroups (131,072 rows of
-  // hidden 64: 128 / 768 / 1,536 workgroups 51 / 41 / 53 us), at most as many as keep a
-  // team's chain of rows and the chains along the partial rows balanced (429 rows of 256:
-  // one row a team 6.3 us, three 9.6, before the partial rows), and at most 32 (131,072
-  // rows of 1,152: 16 / 32 / 64 rows 421 / 407 / 420 us).
-  s.team_rows = 1;
-  while (s.team_rows < kBwdRowsMax && int64_t(64) * s.team_rows * s.team_rows < rows &&
-         int64_t(s.team_rows) * s.teams_of_block * kBwdBlocks < rows)
-    ++s.team_rows;
+  // Rows of a team: the workgroups are one evenly filled round of what fits the chip, or
+  // as few as teams of at most kBwdRowsMax rows (which a lane adds one after another)
+  // allow; two where sequences are short, whose ends cost a team as much as a row and are
+  // not spread evenly, if that leaves a team four rows (65,536 rows of 64: three rows a
+  // team 35 us, two 44).  Long sequences, 131,072 rows of hidden 1,152: 103 / 64 / 52 / 32 /
+  // 16 rows 392 / 411 / 401 / 409 / 429 us; 16,384 rows of 4,096: 64 / 32 / 16 / 8 rows 192
+  // / 197 / 202 / 208.  Sequences of 1 to 51 rows, one round / two: 30,000 rows of 2,048 214
+  // / 192, 16,384 of 4,096 249 / 228, 65,536 of 576 144 / 126, of 1,152 252 / 226 and 211 /
+  // 220.
+  const int64_t round = int64_t(s.teams_of_block) * kNumCU * (4 * bwd_waves(s.lanes) / (s.block / 64));
+  const bool shorts = n_seqs > 0 && rows < int64_t(kShortRows) * n_seqs && rows >= 8 * round;
+  const int64_t least = (rows + round * kBwdRowsMax - 1) / (round * kBwdRowsMax);
+  const int64_t rounds = shorts && least < 2 ? 2 : least > 1 ? least : 1;
+  s.team_rows = rows > 0 ? int((rows + round * rounds - 1) / (round * rounds)) : 1;
   const int64_t per_block = int64_t(s.teams_of_block) * s.team_rows;
   s.blocks = (rows + per_block - 1) / per_block;
   s.teams = s.blocks * s.teams_of_block;
@@ -263,19 +293,16 @@ struct BwdParts {
 };
 
 template <int TL, int FMT, bool DY32>
-__global__ __launch_bounds__(Team<TL>::kBlock) void gated_norm_bwd_kernel(GatedNormBwd p, BwdParts w) {
+__global__ __launch_bounds__(Team<TL>::kBlock, bwd_waves(TL)) void gated_norm_bwd_kernel(GatedNormBwd p, BwdParts w) {
   using T = Team<TL>;
   __shared__ float red[2][3 * (T::kBlock / 64)];
   __shared__ float sums[T::kTeams][8 * TL];
-  const int team = threadIdx.x / TL, lane = threadIdx.x % TL, c = 8 * lane;
+  const int team = T::alike(threadIdx.x / TL), lane = threadIdx.x % TL, c = 8 * lane;
   const int h = p.hidden, groups = (h + kActGroup - 1) / kActGroup;
   const bool mine = c < h;
-  const int64_t block_first = int64_t(blockIdx.x) * T::kTeams * w.team_rows;
-  const int64_t first = block_first + int64_t(team) * w.team_rows;
-  int64_t rows = p.rows;
-  if (p.cu) rows = min(rows, int64_t(p.cu[p.n_seqs]));
-  const int64_t left = rows - (T::kWaves > 1 ? block_first : first);
-  const int turns = int(max(min(left, int64_t(w.team_rows)), int64_t(0)));
+  const row_t rows = rows_of(p.rows, p.cu, p.n_seqs), block_first = blockIdx.x * row_t(T::kTeams * w.team_rows);
+  const row_t first = block_first + row_t(team * w.team_rows), lead = T::kWaves > 1 ? block_first : first;
+  const int turns = lead < rows ? int(min(rows - lead, row_t(w.team_rows))) : 0;
   const bool has_f = p.post != nullptr || p.gate != nullptr;
   const __bf16 *dout = static_cast<const __bf16*>(p.dout);
   const __bf16 *post = static_cast<const __bf16*>(p.post), *gate = static_cast<const __bf16*>(p.gate);
@@ -284,12 +311,12 @@ __global__ __launch_bounds__(Team<TL>::kBlock) void gated_norm_bwd_kernel(GatedN
   f32x4 dn32[2] = {};
   Held8<FMT> fn{}, on{};
   float rfn = 1.f, ron = 0.f;
-  auto fetch = [&](int64_t row) {
+  auto fetch = [&](row_t row) {
     if (row >= rows) return;
     if (p.post) rfn = p.rstd_f[row];
     if (p.pre) ron = p.rstd_out[row];
     if (!mine) return;
-    const int64_t at = row * h + c, grp = row * groups + (c >> 5);
+    const int64_t at = int64_t(row) * h + c, grp = int64_t(row) * groups + (c >> 5);
     if (dout) gn = *reinterpret_cast<const bf16x8*>(dout + at);
     if (p.pre) {
       on.load(p.out, static_cast<const uint8_t*>(p.out_scales), at, grp);
@@ -303,14 +330,15 @@ __global__ __launch_bounds__(Team<TL>::kBlock) void gated_norm_bwd_kernel(GatedN
     if (has_f) fn.load(p.f, static_cast<const uint8_t*>(p.f_scales), at, grp);
   };
   fetch(first);
-  float branch[8], pre[8], acc_pre[8], acc_a[8];  // post o gate, pre; sums of dy o oh, G o fh
-  gains(static_cast<const __bf16*>(p.pre), c, h, pre);
-  Walk walk;
-  walk.s = 0;
-  walk.end = INT64_MAX;
-  int64_t from = first;  // first of the team's rows in the current sequence
-  if (p.cu && first < rows) walk.start<T::kSub>(p.cu, p.n_seqs, first);
-  gains_product(post, gate ? gate + int64_t(walk.s) * h : nullptr, c, h, branch);
+  float acc_pre[8], acc_a[8];  // sums of dy o oh, G o fh
+  bf16x8 post8 = gain8(post, c, h), pre8 = gain8(static_cast<const __bf16*>(p.pre), c, h);
+  Walk<TL> walk;
+  row_t from = first;  // first of the team's rows in the current sequence
+  if (p.cu && first < rows) walk.start(p.cu, p.n_seqs, first);
+  // the gate of the current sequence, and of the next: a short sequence's end waits for
+  // neither offsets nor gates
+  bf16x8 gate8 = gain8(gate ? gate + int64_t(walk.s) * h : nullptr, c, h), gate_next{};
+  if (p.cu) gate_next = gain8(gate + int64_t(min(walk.s + 1, p.n_seqs - 1)) * h, c, h);
   float* sum = &sums[team][c];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
@@ -319,20 +347,17 @@ __global__ __launch_bounds__(Team<TL>::kBlock) void gated_norm_bwd_kernel(GatedN
   }
   // The team's sum of G o fh over rows [from, to) of the current sequence leaves the
   // registers.
-  auto flush = [&](int64_t to) {
+  auto flush = [&](row_t to) {
     if (!mine) return;
-    const bool starts = int64_t(p.cu[walk.s]) >= first, whole = starts && to >= min(walk.end, rows);
+    const bool starts = walk.begin >= first, whole = starts && to >= min(walk.end, rows);
     float* dst = (whole ? p.dgate + int64_t(walk.s) * h
                         : w.seg + ((int64_t(blockIdx.x) * T::kTeams + team) * 2 + (from > first ? 1 : 0)) * h) + c;
-    float g[8], q[8];
-    gains(gate + int64_t(walk.s) * h, c, h, g);
-    gains(post, c, h, q);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      sum[e] += g[e] * acc_a[e];
+      sum[e] += float(gate8[e]) * acc_a[e];
       float v = acc_a[e];
       if (whole) {
-        v *= q[e];
+        v *= float(post8[e]);
         if (p.accumulate) v += dst[e];
       }
       dst[e] = v;
@@ -340,14 +365,18 @@ __global__ __launch_bounds__(Team<TL>::kBlock) void gated_norm_bwd_kernel(GatedN
     }
   };
   for (int i = 0; i < turns; ++i) {
-    const int64_t row = first + i;
+    const row_t row = first + row_t(i);
     const bool live = row < rows;
     if (live && row >= walk.end) {
       flush(row);
       from = row;
-      walk.step(row);
-      gains_product(post, gate + int64_t(walk.s) * h, c, h, branch);
+      gate8 = gate_next;
+      if (walk.step(row) > 1) gate8 = gain8(gate + int64_t(walk.s) * h, c, h);
+      gate_next = gain8(gate + int64_t(min(walk.s + 1, p.n_seqs - 1)) * h, c, h);
     }
+    stay_packed(post8);
+    stay_packed(pre8);
+    stay_packed(gate8);
     float t[8], d[8], oh[8], fh[8];
     const float rf = rfn, ro = ron;
 #pragma unroll
@@ -366,18 +395,18 @@ __global__ __launch_bounds__(Team<TL>::kBlock) void gated_norm_bwd_kernel(GatedN
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       acc_pre[e] += d[e] * oh[e];
-      d[e] *= pre[e];
+      d[e] *= float(pre8[e]);
       t[e] += ro * d[e];
       r[0] += d[e] * oh[e];
-      const float b = branch[e] * fh[e];
+      const float b = float(post8[e]) * float(gate8[e]) * fh[e];
       r[1] += b * t[e];
       r[2] += b * oh[e];
     }
     if (live && mine && p.y) {
       float y[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = oh[e] * pre[e];
-      *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.y) + row * h + c) = rounded(y);
+      for (int e = 0; e < 8; ++e) y[e] = oh[e] * float(pre8[e]);
+      *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.y) + int64_t(row) * h + c) = rounded(y);
     }
     team_total<TL>(r, red[0], i & 1);
     const float m = ro * (r[0] / float(h));
@@ -387,16 +416,16 @@ __global__ __launch_bounds__(Team<TL>::kBlock) void gated_norm_bwd_kernel(GatedN
     for (int e = 0; e < 8; ++e) {
       t[e] -= m * oh[e];  // G
       acc_a[e] += t[e] * fh[e];
-      u[e] = rf * (branch[e] * t[e] - mf * fh[e]);
+      u[e] = rf * (float(post8[e]) * float(gate8[e]) * t[e] - mf * fh[e]);
       t[e] *= p.alpha;
     }
     if (live && mine) {
-      if (p.dx) *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.dx) + row * h + c) = rounded(t);
-      *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.df) + row * h + c) = rounded(u);
+      if (p.dx) *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.dx) + int64_t(row) * h + c) = rounded(t);
+      *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.df) + int64_t(row) * h + c) = rounded(u);
     }
   }
   if (p.cu) {
-    if (first < rows) flush(min(first + w.team_rows, rows));
+    if (first < rows) flush(min(first + row_t(w.team_rows), rows));
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum[e] = acc_a[e];
@@ -483,13 +512,13 @@ __global__ __launch_bounds__(1024) void gated_norm_reduce_kernel(GatedNormBwd p,
     return;
   }
   role -= 2 * g.chunks;
-  const int64_t rows = min(p.rows, int64_t(p.cu[p.n_seqs]));
+  const int64_t rows = rows_of(p.rows, p.cu, p.n_seqs);
   // Sequence s as first team, last team and the partial row of the first.
   struct Span {
     int64_t t0, t1, head;
   };
   auto span = [&](int s) {
-    const int64_t lo = max(int64_t(p.cu[s]), int64_t(0)), hi = min(int64_t(p.cu[s + 1]), rows);
+    const int64_t lo = offset_of(p.cu, s), hi = min(int64_t(offset_of(p.cu, s + 1)), rows);
     Span q{lo / R, (hi - 1) / R, 0};
     q.head = 2 * q.t0 + (lo % R != 0 ? 1 : 0);
     return q;
@@ -518,7 +547,7 @@ __global__ __launch_bounds__(1024) void gated_norm_reduce_kernel(GatedNormBwd p,
     const int64_t t = int64_t(role / g.strips) * kSpan;
     const int part = threadIdx.x / (kLong / 4), col = threadIdx.x % (kLong / 4), c = role % g.strips * kLong + 4 * col;
     if (t * R >= rows) return;
-    const int s = min(sequence_of<64>(p.cu, p.n_seqs, t * R), p.n_seqs - 1);
+    const int s = min(sequence_of<64>(p.cu, p.n_seqs, row_t(t * R)), p.n_seqs - 1);
     const Span q = span(s);
     const int64_t from = q.head - q.t0;  // the first team whose first row it contains
     if (q.t1 - q.t0 <= kSpan || t < from || t >= from + kSpan) return;
@@ -536,7 +565,7 @@ __global__ __launch_bounds__(1024) void gated_norm_reduce_kernel(GatedNormBwd p,
   if (role < g.short_blocks) {
     const int64_t unit = int64_t(role) * kWaves + wave, t = unit / g.wide, next = (t + 1) * R;
     if (next >= rows) return;  // nothing goes on behind team t
-    const int s = min(sequence_of<64>(p.cu, p.n_seqs, next), p.n_seqs - 1);
+    const int s = min(sequence_of<64>(p.cu, p.n_seqs, row_t(next)), p.n_seqs - 1);
     const Span q = span(s);
     if (q.t0 != t || q.t1 == t || q.t1 - t > kSpan) return;
     const int c = int(unit % g.wide) * kWide + 4 * lane;
@@ -547,7 +576,7 @@ __global__ __launch_bounds__(1024) void gated_norm_reduce_kernel(GatedNormBwd p,
   if (p.accumulate) return;
   const int64_t s = int64_t(role) * 1024 + threadIdx.x;
   bool none = false;
-  if (s < p.n_seqs) none = min(int64_t(p.cu[s + 1]), rows) <= max(int64_t(p.cu[s]), int64_t(0));
+  if (s < p.n_seqs) none = min(int64_t(offset_of(p.cu, int(s) + 1)), rows) <= int64_t(offset_of(p.cu, int(s)));
   for (uint64_t left = __ballot(none); left; left &= left - 1) {
     float* dst = p.dgate + (s - lane + __ffsll(static_cast<unsigned long long>(left)) - 1) * h;
     for (int c = lane; c < h; c += 64) dst[c] = 0.f;
@@ -600,12 +629,12 @@ hipError_t launch_gated_norm_fwd(const GatedNormFwd& p, hipStream_t s) {
 }
 
 size_t gated_norm_bwd_workspace(int64_t rows, int hidden, int n_seqs) {
-  const BwdShape b = bwd_shape(rows, hidden);
+  const BwdShape b = bwd_shape(rows, hidden, n_seqs);
   return 2 * up256(4 * size_t(b.blocks) * size_t(hidden)) + (n_seqs ? up256(8 * size_t(b.teams) * size_t(hidden)) : 0);
 }
 
 hipError_t launch_gated_norm_bwd(const GatedNormBwd& p, void* workspace, hipStream_t s) {
-  const BwdShape b = bwd_shape(p.rows, p.hidden);
+  const BwdShape b = bwd_shape(p.rows, p.hidden, p.cu ? p.n_seqs : 0);
   char* ws = static_cast<char*>(workspace);
   const size_t part = up256(4 * size_t(b.blocks) * size_t(p.hidden));
   const BwdParts w{reinterpret_cast<float*>(ws), reinterpret_cast<float*>(ws + part),

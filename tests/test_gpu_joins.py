@@ -8,8 +8,8 @@ a lane, 2-3 chunks, 6 lane steps and 4 wavefronts, a result takes some ten furth
 operations, in all fewer than 64 roundings of 2^-24: 2^-18 of the terms' sum, plus
 the hardware's exp, reciprocal and reciprocal root (1 ulp each, 2^-23, and e^x's
 argument below 2^8 with 2^-24 of itself: 2^-16).  2^-15 of the magnitudes covers
-both.  Weight gradients are fp32 sums over rows: up to 64 rows in a lane, 4 teams,
-and partial rows 32 apart in four running sums, below 2^9 roundings for the sizes
+both.  Weight gradients are fp32 sums over rows: up to 128 rows in a lane, 32 teams,
+and partial rows 32 apart in eight running sums, below 2^9 roundings for the sizes
 here: 2^-15 of the sum of magnitudes; where the terms come from bf16 inputs
 nothing else is lost."""
 
