@@ -8,6 +8,8 @@ Modules
 -------
 attention : float64 numpy block-diagonal (packed) exact self-attention,
             forward and analytic backward, plus row-sampled variants.
+layer     : float64 transformer layer around it; join, block: the gated, normed
+            join and the block made of both; checkpoint: 8-bit activations.
 planner   : Python-int DCP planner (DCP-intra, DCP-inter, gradient
             accumulation search) and exhaustive brute-force searches.
 """

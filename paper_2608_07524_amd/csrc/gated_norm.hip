@@ -12,11 +12,11 @@
 //   dpre = sum_t dy o oh.
 // HBM-bound: every input is read once and every output written once, all of a row
 // in registers between; sums, statistics and gradients of the parameters are fp32.
-// 131,072 rows of hidden 1,152, eight sequences, int8: join with f's checkpoint 262
-// us (5.2 TB/s), backward 382 + 28 (4.8 TB/s and the partial rows), a 2 GiB copy 4.92
-// TB/s.  65,536 rows in 4,000 sequences of 1 to 51 tokens: 205 + 17.  16,384 rows of
-// hidden 4,096 in bf16: join 98 (5.5), backward 187 + 11 (5.0).  429 rows of 256: 3.9;
-// 6.3 + 5.6, chains of memory latencies.
+// 131,072 rows of hidden 1,152, eight sequences, int8: join with f's checkpoint 257
+// us (5.3 TB/s), backward 384 + 12 (4.7 TB/s, and the partial rows), a 2 GiB copy 4.92
+// TB/s.  65,536 rows in 4,000 sequences of 1 to 51 tokens: 199 + 21.  16,384 rows of
+// hidden 4,096 in bf16: join 98 (5.5), backward 190 + 5 (4.9).  429 rows of 256: 3.7;
+// 5.6 + 5.7, chains of memory latencies.
 #include <type_traits>
 
 #include "act8.h"
@@ -28,9 +28,9 @@ namespace {
 
 // A team of TL lanes owns a row, 8 columns (one 16-byte access) a lane: the power
 // of two up to 64, or the multiple of 64, that covers hidden / 8.  One piece a lane
-// keeps the backward at a hundred registers, so that four wavefronts share a SIMD and
-// loads are always in flight; with three pieces (one wavefront for hidden 1,152) it
-// took 259, one wavefront a SIMD, and twice the time.  Teams take consecutive rows:
+// keeps the backward at 128 registers, so that four wavefronts share a SIMD and loads
+// are always in flight; with three pieces (one wavefront for hidden 1,152) it took 259,
+// one wavefront a SIMD, and twice the time.  Teams take consecutive rows:
 // gains, gate and the place in cu_seqlens are fetched once, and the next row is
 // loaded before the present one is worked on.  A workgroup is one team of more than
 // 128 lanes or 256 lanes of smaller ones (two teams of 192: 12 wavefronts a CU instead

@@ -298,9 +298,9 @@ def _case(torch, P, lengths, h, gate, post, pre, fmt, f32, alpha=1.0, extra=0, s
 # across two, and over more teams than a workgroup's parts (32 of 4 rows).
 @pytest.mark.parametrize("fmt", ["bf16", "int8", "e4m3"])
 @pytest.mark.parametrize("h,lengths", [(8, [1]), (72, [0, 5, 0, 0, 1, 30, 0]), (256, [37, 64, 128, 200]),
-                                       (520, [3, 4, 4, 1]), (1024, [9]), (1152, [1, 700, 16, 16, 33]),
+                                       (288, [2, 90, 1]), (512, [7]), (520, [3, 4, 4, 1]), (1024, [9]), (1152, [1, 700, 16, 16, 33]),
                                        (1536, [2, 7]), (1544, [40, 1, 200]), (2048, [6]), (2304, [5, 150]),
-                                       (3080, [3, 0, 140]), (4096, [1, 21])])
+                                       (2600, [30, 31]), (3080, [3, 0, 140]), (4096, [1, 21])])
 def test_join_over_widths(torch, P, fmt, h, lengths):
     _case(torch, P, lengths, h, "sequence", True, True, fmt, False, extra=3)
 
