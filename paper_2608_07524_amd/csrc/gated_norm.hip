@@ -14,7 +14,7 @@
 // in registers between; sums, statistics and gradients of the parameters are fp32.
 // 131,072 rows of hidden 1,152, eight sequences, int8: join with f's checkpoint 257
 // us (5.3 TB/s), backward 384 + 12 (4.7 TB/s, and the partial rows), a 2 GiB copy 4.92
-// TB/s.  65,536 rows in 4,000 sequences of 1 to 51 tokens: 199 + 21.  16,384 rows of
+// TB/s.  65,536 rows in 1,286 sequences of 1 to 51 tokens: 198 + 12.  16,384 rows of
 // hidden 4,096 in bf16: join 98 (5.5), backward 190 + 5 (4.9).  429 rows of 256: 3.7;
 // 5.6 + 5.7, chains of memory latencies.
 #include <type_traits>
@@ -260,7 +260,7 @@ inline int team_lanes(int hidden) {
 // Wavefronts that share a SIMD: 128 registers each where a team's rows and offsets are in
 // scalar registers, more otherwise.
 constexpr int bwd_waves(int lanes) { return lanes < 64 ? 3 : 4; }
-constexpr int kBwdRowsMax = 128, kShortRows = 64;
+constexpr int kBwdRowsMax = 128, kShortRows = 32;
 inline BwdShape bwd_shape(int64_t rows, int hidden, int n_seqs) {
   BwdShape s;
   s.lanes = team_lanes(hidden);
@@ -272,9 +272,9 @@ inline BwdShape bwd_shape(int64_t rows, int hidden, int n_seqs) {
   // not spread evenly, if that leaves a team four rows (65,536 rows of 64: three rows a
   // team 35 us, two 44).  Long sequences, 131,072 rows of hidden 1,152: 103 / 64 / 52 / 32 /
   // 16 rows 392 / 411 / 401 / 409 / 429 us; 16,384 rows of 4,096: 64 / 32 / 16 / 8 rows 192
-  // / 197 / 202 / 208.  Sequences of 1 to 51 rows, one round / two: 30,000 rows of 2,048 214
-  // / 192, 16,384 of 4,096 249 / 228, 65,536 of 576 144 / 126, of 1,152 252 / 226 and 211 /
-  // 220.
+  // / 197 / 202 / 208.  Sequences of 1 to 51 rows, one round / two: on average 17 to 23
+  // rows, 30,000 rows of 2,048 214 / 192, 16,384 of 4,096 249 / 228, 65,536 of 576 144 /
+  // 126, of 1,152 252 / 226; on average 51, 65,536 of 1,152 211 / 219.
   const int64_t round = int64_t(s.teams_of_block) * kNumCU * (4 * bwd_waves(s.lanes) / (s.block / 64));
   const bool shorts = n_seqs > 0 && rows < int64_t(kShortRows) * n_seqs && rows >= 8 * round;
   const int64_t least = (rows + round * kBwdRowsMax - 1) / (round * kBwdRowsMax);
@@ -457,9 +457,9 @@ __global__ __launch_bounds__(Team<TL>::kBlock, bwd_waves(TL)) void gated_norm_bw
 //  - short: one wavefront for each team t and 256 columns, for the sequence, if any,
 //    that starts in t and ends at most kSpan teams later;
 //  - empty: zeros for the sequences without rows.
-// (With a list of the sequences for every 32 columns: 79 us for 4,000 sequences of 1 to
+// (With a list of the sequences for every 32 columns: 79 us for 1,286 sequences of 1 to
 // 51 tokens, hidden 1,152; long ones one after another in 32 columns: 65 us for 32,768
-// rows of hidden 4,096 in 50 sequences.)
+// rows of hidden 4,096 in 42 sequences.)
 constexpr int kCols = 32, kParts = 32, kSpan = 32, kLong = 128, kWaves = 16, kWide = 256;
 constexpr int kRuns = 8;  // loads in flight along a column (4 along a short sequence's)
 
