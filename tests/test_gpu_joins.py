@@ -464,3 +464,20 @@ def test_join_on_other_streams(torch, P):
     torch.cuda.synchronize()
     for a, b in zip(want, got):
         assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_join_keeps_either(torch, P, fmt):
+    """A checkpoint of out alone, of f alone, and with no norm or gate at all: those of
+    the matrices themselves."""
+    rng = np.random.default_rng(10)
+    for h in (72, 1152):
+        x, f = (to_device(torch, _bits(rng.standard_normal((33, h)))) for _ in range(2))
+        g = torch.ones(h, dtype=torch.bfloat16, device="cuda")
+        for w in (dict(), dict(pre=g), dict(post=g, gate=g, pre=g)):
+            for keep in (dict(keep_out=fmt), dict(keep_f=fmt)):
+                r = P.gated_norm_fwd(x, f, residual_scale=0.5, **w, **keep)
+                got, of = (r.out8, r.out) if "keep_out" in keep else (r.f8, f)
+                assert (r.f8 is None) == ("keep_out" in keep) and (r.out8 is None) == ("keep_f" in keep)
+                for a, b in zip(got, P.act8_pack(of, fmt)):
+                    assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
