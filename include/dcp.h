@@ -618,15 +618,17 @@ int dcp_gated_norm_bwd(const dcp_gated_norm_desc* desc, const dcp_gated_norm_wei
  * with the join of dcp_gated_norm_fwd: h = residual_scale x + gate1 o RMSNorm(o Wo;
  * post1).  Without post norms, gates and with residual_scale 1 it is the layer's
  * function.
- * The stash holds q, k, v, o, h and u, with post norms or gates also the two
- * branches' outputs, in stash_format (see dcp_act8_desc), and the LSE and row scales in
- * fp32: 9 or 11 elements a token and hidden column, where the layer's stash holds 15
- * in bf16 (y1, y2 and a are formed again in the backward).  An 8-bit stash changes
- * the gradients by its rounding, not the output; a recomputing backward (stash NULL)
- * forms everything again in bf16.
+ * The stash holds q, k, v, h and u, with post norms or gates also the two branches'
+ * outputs, in stash_format (see dcp_act8_desc), o in bf16 (its gradient's row sums have
+ * to cancel), and the LSE and row scales in fp32: 9 or 11 elements a token and hidden
+ * column, where the layer's stash holds 15 in bf16 (y1, y2 and a are formed again in
+ * the backward).  An 8-bit stash changes the gradients by its rounding, not the output:
+ * the attention's weights, for one, are formed again from q and k as held against the
+ * LSE of the forward, each off by the factor e^(what its logit moved), so that large
+ * logits want int8.  A recomputing backward (stash NULL) forms everything again in bf16.
  *   Layout of the stash, each part at the next multiple of 256 bytes: q, k, v, o,
- * o Wo (with post norms or gates), h, a Wdown (likewise), u -- each bf16, or its codes
- * and then its scale bytes -- then the LSE [n_heads, T] and 1 / rms of o Wo, h and
+ * o Wo (with post norms or gates), h, a Wdown (likewise), u -- each bf16, or, all but o,
+ * its codes and then its scale bytes -- then the LSE [n_heads, T] and 1 / rms of o Wo, h and
  * a Wdown [T], fp32 (unused ones too).
  */
 enum { DCP_GATE_NONE = 0, DCP_GATE_SHARED = 1, DCP_GATE_SEQUENCE = 2 };

@@ -9,7 +9,7 @@
 
 namespace dcp {
 
-constexpr int kActMax = 4;  // matrices of one pack or unpack launch (Q, K, V and O of a layer)
+constexpr int kActMax = 3;  // matrices of one pack or unpack launch (Q, K and V of a layer)
 struct ActBatch {
   const void* src[kActMax];  // bf16 (pack) or codes (unpack)
   void* dst[kActMax];        // codes (pack) or bf16 (unpack)

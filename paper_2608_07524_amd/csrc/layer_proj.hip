@@ -17,7 +17,7 @@
 // K and V 145 us, W_up with GELU 201, dY1 137 (eight wavefronts with 256 x 256
 // tiles, 192 x 256 tiles, and reading the next slice's first operands across the
 // barrier: 1-40 % slower); library and fused times at the layer's sizes stand at
-// the rules in layer_api.cpp.
+// the rules in layer_internal.h.
 #include <type_traits>
 
 #include "act8.h"

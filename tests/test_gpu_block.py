@@ -74,7 +74,7 @@ def _stash(torch, block, fmt, H, branch):
     kept = {}
     for name in ("q", "k", "v", "o") + (("f1",) if branch else ()) + ("h",) + (("f2",) if branch else ()) + ("u",):
         cols = 4 * h if name == "u" else h
-        if fmt == "bf16":
+        if fmt == "bf16" or name == "o":
             t = take(2 * T * cols, torch.bfloat16, (T, cols))
         else:
             codes = take(T * cols, torch.int8 if fmt == "int8" else torch.float8_e4m3fn, (T, cols))
@@ -101,7 +101,7 @@ def _errors(torch, block, cu, W, host, dev, H, D, causal, fmt, alpha):
             top = np.max(np.abs(kept[n]))
             # (the half step of a group is at most that of the largest magnitude: 1 / 127 of
             # it, or 2^-4; with what the products moved, 1.02 of it)
-            half = {"bf16": 0.0, "int8": 1.02 / 127, "e4m3": 1.02 / 16}[fmt] * top
+            half = {"bf16": 0.0, "int8": 1.02 / 127, "e4m3": 1.02 / 16}["bf16" if n == "o" else fmt] * top
             assert np.max(np.abs(held[n] - kept[n])) <= GRAD_TOL * top + half, n
     for n in ("f1", "f2"):
         held.setdefault(n, None)
@@ -111,13 +111,8 @@ def _errors(torch, block, cu, W, host, dev, H, D, causal, fmt, alpha):
     rel = lambda a, b: float(np.max(np.abs(a - b)) / np.max(np.abs(b)))
     errs = {"out": rel(I.bf16_to_f64(to_bits(out)), ref), "dx": rel(I.bf16_to_f64(to_bits(dx)), rdx)}
     got = {n: g.double().cpu().numpy() for n, g in block.grads.items()}
-    for n in ("wq", "wk"):
-        # A softmax over one key has no gradient; the kernels' and the oracle's are what dO . v
-        # and dO . o, equal sums of up to 128 products, leave over: below 2^7 2^-24 of terms
-        # that wv's gradient is made of too, times keys and queries of order 1.
-        if len(dx) == 1:
-            assert np.max(np.abs(rg[n])) < 1e-12 and np.max(np.abs(got[n])) <= 2.0 ** -12 * np.max(np.abs(got["wv"])), n
-            del rg[n]
+    # (one token, whose query and key have no gradient, is given what v's rounding leaves of
+    # dO . v - dO . o: the same on both sides)
     errs.update({n: rel(got[n], rg[n]) for n in rg})
     print(f"block {fmt} H={H} D={D} T={len(dx)}: " + " ".join(f"{k} {v:.1e}" for k, v in errs.items()), flush=True)
     return errs
@@ -284,3 +279,23 @@ def test_stack_of_blocks(torch, gated):
     rows = {fmt: M.profile_rows([256], 2, 64, True, reps=2, warmup=1, stash_format=fmt, **kind)[0] for fmt in
             ("bf16", "int8")}
     assert rows["int8"].m_bytes < 0.6 * rows["bf16"].m_bytes and rows["int8"].t_f_ns > 0
+
+
+def test_eight_bit_gradients_are_near(torch):
+    """Through a stack of blocks the gradients from 8-bit stashes stay near those from
+    bf16, in the first block as in the last: relative errors of the order of the formats'
+    own (0.8 % of the standard deviation, 2.7 %), at most four times that.  (A query's or
+    key's gradient multiplies three held matrices, its noise adds in quadrature, sqrt(3) of
+    one; the weights' e^(logit) adds as much again, and inputs and dY1 carry the later
+    blocks' errors.  With o in 8 bits dWq of the last block is off by 7 and 23 %.)"""
+    from paper_2608_07524_amd import model as M
+    res = {}
+    for fmt in ("bf16", "int8", "e4m3"):
+        st = M.Stack(4, [0, 1024, 2048, 4096], 16, 72, False, seed=3, stash_format=fmt, post_norm=True, gates=3)
+        st.step([0] * 4)
+        torch.cuda.synchronize()
+        res[fmt] = [st.dys[0].float()] + [layer.grads[n].clone() for layer in st.layers for n in layer.grads]
+    for fmt, own in (("int8", 0.0083), ("e4m3", 0.027)):
+        errs = [float((a - b).norm() / b.norm()) for a, b in zip(res[fmt], res["bf16"])]
+        print(f"{fmt}: " + " ".join(f"{e:.4f}" for e in errs), flush=True)
+        assert max(errs) <= 4 * own
