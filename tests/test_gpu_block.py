@@ -299,3 +299,28 @@ def test_eight_bit_gradients_are_near(torch):
         errs = [float((a - b).norm() / b.norm()) for a, b in zip(res[fmt], res["bf16"])]
         print(f"{fmt}: " + " ".join(f"{e:.4f}" for e in errs), flush=True)
         assert max(errs) <= 4 * own
+
+
+def test_wide_block_of_many_tokens(torch):
+    """Hidden 4,096 from 12,288 tokens on: the library's weight gradients, and no fused
+    products; the sum of the gradients of the batch's halves."""
+    import paper_2608_07524_amd as P
+    H, D, T = 32, 128, 12288
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    rand = lambda *s: torch.randn(*s, generator=gen, device="cuda")
+    W = {n: (rand(*s) / (math.sqrt(s[0]) if n.startswith("w") else 1.0)).to(torch.bfloat16)
+         for n, s in P.block_param_shapes(H * D, True, 1).items()}
+    x, dout = (rand(T, H * D).to(torch.bfloat16) for _ in range(2))
+
+    def grads(rows):
+        g = {n: torch.zeros(w.shape, dtype=torch.float32, device="cuda") for n, w in W.items()}
+        for lo in range(0, T, rows):
+            block = P.Block(W, g, np.arange(0, rows + 1, 512), H, D, True, None, 1e-6, stash_format="int8")
+            block.fwd(x[lo:lo + rows])
+            block.bwd(x[lo:lo + rows], dout[lo:lo + rows])
+            torch.cuda.synchronize()
+        return g
+
+    whole, halves = grads(T), grads(T // 2)
+    errs = {n: float((whole[n] - halves[n]).abs().max() / halves[n].abs().max()) for n in W}
+    assert max(errs.values()) <= GRAD_TOL, errs
