@@ -155,6 +155,9 @@ __device__ __forceinline__ bf16x8 rounded(const float (&v)[8]) {
   return b;
 }
 
+// v where the mask is all ones, 0 (also for a NaN) where it is zero.
+__device__ __forceinline__ float masked(float v, uint32_t mask) { return __uint_as_float(__float_as_uint(v) & mask); }
+
 template <int FMT>
 __device__ __forceinline__ void keep8(void* codes, void* scales, bf16x8 v, row_t row, int c, int h, int groups) {
   const uint32_t byte = scale_byte<FMT>(group_top(top_bits(v)));
@@ -304,6 +307,9 @@ __global__ __launch_bounds__(Team<TL>::kBlock, bwd_waves(TL)) void gated_norm_bw
   const row_t first = block_first + row_t(team * w.team_rows), lead = T::kWaves > 1 ? block_first : first;
   const int turns = lead < rows ? int(min(rows - lead, row_t(w.team_rows))) : 0;
   const bool has_f = p.post != nullptr || p.gate != nullptr;
+  // (without post df = gate o G, whatever f holds: 0 fh would be NaN where f is not finite; a
+  // branch instead of the mask spills registers from 64 lanes on)
+  const uint32_t normed = p.post ? ~0u : 0u;
   const __bf16 *dout = static_cast<const __bf16*>(p.dout);
   const __bf16 *post = static_cast<const __bf16*>(p.post), *gate = static_cast<const __bf16*>(p.gate);
 
@@ -416,7 +422,7 @@ __global__ __launch_bounds__(Team<TL>::kBlock, bwd_waves(TL)) void gated_norm_bw
     for (int e = 0; e < 8; ++e) {
       t[e] -= m * oh[e];  // G
       acc_a[e] += t[e] * fh[e];
-      u[e] = rf * (float(post8[e]) * float(gate8[e]) * t[e] - mf * fh[e]);
+      u[e] = rf * (float(post8[e]) * float(gate8[e]) * t[e] - mf * masked(fh[e], normed));
       t[e] *= p.alpha;
     }
     if (live && mine) {

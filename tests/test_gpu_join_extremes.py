@@ -1,0 +1,85 @@
+"""Joins of a branch without a norm, whose values may be as large as bf16 holds, or
+not finite: what by definition does not depend on them does not change, what does is
+the definition's sum.
+
+Tolerance: the results here are products and sums of at most 8 rows in fp32, fewer than
+16 roundings of 2^-24 of the magnitudes added: 2^-20 of them."""
+
+import numpy as np
+import pytest
+
+from oracle import join as J
+from paper_2608_07524_amd import inputs as I
+
+from gpu_util import to_bits, to_device
+
+pytestmark = pytest.mark.gpu
+
+LENGTHS = [3, 0, 5]
+
+
+@pytest.fixture(scope="module")
+def torch():
+    t = pytest.importorskip("torch")
+    if not t.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2608_07524_amd as P
+    P.load()
+    return t
+
+
+@pytest.fixture(scope="module")
+def P(torch):
+    import paper_2608_07524_amd as P
+    return P
+
+
+def _bits(a):
+    return I.bf16_bits(np.asarray(a, dtype=np.float32))
+
+
+def _gate(torch, rng, kind, h):
+    bits = _bits(rng.standard_normal((len(LENGTHS), h) if kind == "sequence" else h))
+    cu = I.cu_from_lengths(LENGTHS)
+    return to_device(torch, bits), I.bf16_to_f64(bits), cu if kind == "sequence" else None
+
+
+def _held(P, f, fmt):
+    """(what gated_norm_bwd takes, the bf16 values it stands for)."""
+    if fmt == "bf16":
+        return f, f
+    kept = P.act8_pack(f, fmt)
+    return kept, P.act8_unpack(*kept)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "int8", "e4m3"])
+@pytest.mark.parametrize("kind", ["shared", "sequence"])
+@pytest.mark.parametrize("pre", [False, True])
+@pytest.mark.parametrize("h", [72, 1152])
+def test_branch_gradient_without_norm_is_free_of_the_branch(torch, P, fmt, kind, pre, h):
+    """df = gate o G: infinities and NaN in f leave it, and the gate's gradient of the
+    columns and sequences that hold none, as they are."""
+    rng = np.random.default_rng(h)
+    gate, gate64, cu = _gate(torch, rng, kind, h)
+    clean, out, dout, dy = (to_device(torch, _bits(rng.standard_normal((sum(LENGTHS), h)))) for _ in range(4))
+    f = clean.clone()
+    f[1, 3], f[2, h - 1], f[6, 33] = float("inf"), float("nan"), float("-inf")
+    rest = dict(gate=gate, cu_seqlens=cu)
+    if pre:
+        scale = torch.from_numpy(rng.uniform(0.5, 2.0, sum(LENGTHS)).astype(np.float32)).cuda()
+        rest.update(pre=to_device(torch, _bits(1 + 0.2 * rng.standard_normal(h))), rstd_out=scale, dy=dy,
+                    out=_held(P, out, fmt)[0])
+    kept, values = _held(P, f, fmt)
+    got = P.gated_norm_bwd(dout, f=kept, **rest)
+    want = P.gated_norm_bwd(dout, f=_held(P, clean, fmt)[0], **rest)
+    assert torch.equal(got.df, want.df) and torch.equal(got.dx, want.dx)
+    if not pre:  # one rounded product
+        rows = J._gate_rows(gate64, cu, sum(LENGTHS))
+        assert np.array_equal(to_bits(got.df), _bits(rows * I.bf16_to_f64(to_bits(dout))))
+    bad = ~torch.isfinite(values)
+    if cu is None:
+        touched = bad.any(0)
+    else:
+        touched = torch.stack([bad[a:b].any(0) for a, b in zip(cu[:-1], cu[1:])])
+    assert bool(touched.any()) and torch.equal(got.dgate[~touched], want.dgate[~touched])
+    assert not bool(torch.isfinite(got.dgate[touched]).any())
