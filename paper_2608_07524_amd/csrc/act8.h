@@ -132,8 +132,8 @@ __device__ __forceinline__ void decode8(u32x2 c, uint32_t b, float (&x)[8]) {
   }
 }
 
-// The same times m, rounded once (|code 2^k m| far below 2^121: the int8 form passes
-// 128 2^k m).
+// The same times m, rounded once, for 2^k m below 2^121: int8 passes 128 2^k m.  A row's
+// scale 1 / rms holds that, being 0 in fp32 where k is 121 or 122; m = 1 does not.
 template <int FMT>
 __device__ __forceinline__ void decode8_scaled(u32x2 c, uint32_t b, float m, float (&x)[8]) {
   if constexpr (FMT == DCP_ACT_INT8) {

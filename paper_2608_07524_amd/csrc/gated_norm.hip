@@ -391,7 +391,8 @@ __global__ __launch_bounds__(Team<TL>::kBlock, bwd_waves(TL)) void gated_norm_bw
       d[e] = DY32 ? dn32[e >> 2][e & 3] : float(dn[e]);
     }
     on.get_scaled(ro, oh);
-    fn.get_scaled(rf, fh);
+    if (FMT == DCP_ACT_INT8 && !p.post) fn.get(fh);
+    else fn.get_scaled(rf, fh);
     if (!mine || !live) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) t[e] = d[e] = oh[e] = fh[e] = 0.f;

@@ -83,3 +83,28 @@ def test_branch_gradient_without_norm_is_free_of_the_branch(torch, P, fmt, kind,
         touched = torch.stack([bad[a:b].any(0) for a, b in zip(cu[:-1], cu[1:])])
     assert bool(touched.any()) and torch.equal(got.dgate[~touched], want.dgate[~touched])
     assert not bool(torch.isfinite(got.dgate[touched]).any())
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "int8", "e4m3"])
+@pytest.mark.parametrize("kind", ["shared", "sequence"])
+def test_gate_gradient_of_large_branches(torch, P, fmt, kind):
+    """The gate's gradient is G o f summed, with f as its checkpoint reads back: groups of
+    finite values beyond 127 2^120 keep their zeros, small values and signs."""
+    h = 72
+    rng = np.random.default_rng(5)
+    gate, gate64, cu = _gate(torch, rng, kind, h)
+    f64 = rng.standard_normal((sum(LENGTHS), h))
+    # (e4m3: from 248 2^120 = 3.297e38 on a value rounds to 256 2^120 = 2^128)
+    f64[0, 5], f64[2, 40], f64[4, 5], f64[6, 71], f64[5, 0] = 2e38, -3e38, -1.9e38, 3.2e38, 1.7e38
+    f64[3, :32] = 0.0
+    f64[3, 1] = 2.5e38
+    f = to_device(torch, _bits(f64))
+    dout = to_device(torch, _bits(2.0 ** -30 * rng.standard_normal((sum(LENGTHS), h))))
+    kept, values = _held(P, f, fmt)
+    v64 = I.bf16_to_f64(to_bits(values))
+    assert np.all(np.isfinite(v64)) and np.max(np.abs(v64)) > 2e38
+    b = P.gated_norm_bwd(dout, f=kept, gate=gate, cu_seqlens=cu)
+    g, mag = J.backward(I.bf16_to_f64(to_bits(dout)), None, v64, None, None, None, gate=gate64, cu=cu)
+    got, mags = b.dgate.double().cpu().numpy(), mag["dgate"].reshape(b.dgate.shape)
+    assert np.all(np.abs(got - g["dgate"].reshape(got.shape)) <= 2.0 ** -20 * mags)
+    assert np.array_equal(to_bits(b.df), _bits(g["df"]))
