@@ -485,7 +485,9 @@ enum { DCP_ACT_BF16 = 0, DCP_ACT_INT8 = 1, DCP_ACT_E4M3 = 2 };
  *           >= cols (a slice of a wider matrix; columns outside are not touched).
  *   format  DCP_ACT_INT8 or DCP_ACT_E4M3 (DCP_ACT_BF16: dcp_act8_gelu_bwd only).
  * bf16 and fp32 pointers are 16-byte aligned, codes 8-byte.  The calls only
- * enqueue one kernel on `stream` (they may be captured into a graph).
+ * enqueue one kernel on `stream` (they may be captured into a graph).  A buffer that a
+ * call of this section or the next writes may share no byte with another buffer of the
+ * call, except as its description allows (DCP_ERR_INVALID).
  */
 typedef struct {
   int64_t rows;
@@ -594,10 +596,11 @@ typedef struct {
  *   dx    may be NULL (residual_scale 1 and no pre: it would equal dout).
  *   y     may be NULL; needs pre.
  * A gate's gradient is summed over its sequence's rows (0 for an empty one), or
- * over all rows where one gate serves all.  Sums are fp32, in an order fixed by rows,
- * hidden and the offsets: results are bitwise reproducible.  dx or df may be dout's buffer, y, dx
- * or df a bf16 dy's.  The three gradients are distinct buffers.  Two calls that
- * overlap in time need two workspaces.
+ * over all rows where one gate serves all.  Sums are fp32, in an order fixed by
+ * rows, hidden and the offsets: results are bitwise reproducible.  dx, df and y,
+ * distinct, may be the buffers of dout, of a bf16 dy and of f and out as kept in
+ * bf16.  The three gradients are distinct buffers.  Two calls that overlap in time
+ * need two workspaces.
  */
 int dcp_gated_norm_bwd(const dcp_gated_norm_desc* desc, const dcp_gated_norm_weights* w, const void* dout,
                        const void* dy, const dcp_kept* f, const dcp_kept* out, const float* rstd_f,

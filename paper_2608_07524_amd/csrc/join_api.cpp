@@ -8,6 +8,7 @@
 
 #include "api_internal.h"
 #include "block_launch.h"
+#include "buffers.h"
 #include "dcp_internal.h"
 
 namespace dcp {
@@ -59,6 +60,48 @@ int check_join(const dcp_gated_norm_desc* d, const dcp_gated_norm_weights* w) {
   return DCP_OK;
 }
 
+// Buffers of a call on checkpoints: its bf16 matrices, and a checkpoint's two parts.
+Buffer matrix(const dcp_act8_desc* d, const void* p, bool written) {
+  const Buffer::Kind kind = written ? Buffer::kActsWritten : Buffer::kActsRead;
+  if (d->ld == d->cols) return {p, kind, 2 * size_t(d->rows) * size_t(d->cols)};
+  return {p, kind, 2 * size_t(d->cols), d->rows, 2 * size_t(d->ld)};
+}
+Buffer codes_of(const dcp_act8_desc* d, const void* p, bool written) {
+  return {p, written ? Buffer::kWritten : Buffer::kRead, size_t(d->rows) * size_t(d->cols)};
+}
+Buffer scales_of(const dcp_act8_desc* d, const void* p, bool written) {
+  return {p, written ? Buffer::kWritten : Buffer::kRead, size_t(d->rows) * size_t(act_groups(d->cols))};
+}
+
+int apart(std::initializer_list<Buffer> all) {
+  const Buffer* b = clash(all);
+  if (b) return fail(DCP_ERR_INVALID, "the output at %p shares memory with another buffer of the call", b->p);
+  return DCP_OK;
+}
+
+// Buffers of a join.
+struct JoinBuffers {
+  const dcp_gated_norm_desc* d;
+  size_t rows = size_t(d->rows), h = size_t(d->hidden);
+  Buffer read(const void* p) const { return {p, Buffer::kActsRead, 2 * rows * h}; }
+  Buffer written(const void* p) const { return {p, Buffer::kActsWritten, 2 * rows * h}; }
+  Buffer row_scales(const float* p, bool out) const { return {p, out ? Buffer::kWritten : Buffer::kRead, 4 * rows}; }
+  // a kept activation's data and scale bytes
+  Buffer data(const dcp_kept* k, bool out) const {
+    const void* p = k ? k->data : nullptr;
+    if (d->keep_format == DCP_ACT_BF16) return out ? written(p) : read(p);
+    return {p, out ? Buffer::kWritten : Buffer::kRead, rows * h};
+  }
+  Buffer scales(const dcp_kept* k, bool out) const {
+    const bool has = k && k->data && d->keep_format != DCP_ACT_BF16;
+    return {has ? k->scales : nullptr, out ? Buffer::kWritten : Buffer::kRead, rows * size_t(act_groups(d->hidden))};
+  }
+  size_t gates() const { return d->n_seqs > 0 ? size_t(d->n_seqs) : 1; }
+  Buffer weight(const void* p, size_t n) const { return {p, Buffer::kRead, 2 * n * h}; }
+  Buffer grad(const float* p, size_t n) const { return {p, Buffer::kWritten, 4 * n * h}; }
+  Buffer offsets() const { return {d->cu_seqlens, Buffer::kRead, 4 * (size_t(d->n_seqs) + 1)}; }
+};
+
 // A kept activation as an operand: 16-byte aligned bf16, or codes (8-byte) and bytes.
 int check_kept(const dcp_kept* k, int format, const char* what) {
   if (!k) return fail(DCP_ERR_INVALID, "%s is null", what);
@@ -86,6 +129,7 @@ extern "C" int dcp_act8_pack(const dcp_act8_desc* d, const void* x, void* codes,
   DCP_TRY(aligned({x}, 16, "x"));
   DCP_TRY(aligned({codes}, 8, "codes"));
   DCP_TRY(aligned({scales}, 1, "scales"));
+  DCP_TRY(apart({matrix(d, x, false), codes_of(d, codes, true), scales_of(d, scales, true)}));
   DCP_TRY(check_device());
   const ActBatch b{{x}, {codes}, {scales}, 1};
   return launched(launch_act8_pack(b, d->format, d->rows, d->cols, d->ld, static_cast<hipStream_t>(stream)));
@@ -98,6 +142,7 @@ extern "C" int dcp_act8_unpack(const dcp_act8_desc* d, const void* codes, const 
   DCP_TRY(aligned({x}, 16, "x"));
   DCP_TRY(aligned({codes}, 8, "codes"));
   DCP_TRY(aligned({scales}, 1, "scales"));
+  DCP_TRY(apart({matrix(d, x, true), codes_of(d, codes, false), scales_of(d, scales, false)}));
   DCP_TRY(check_device());
   const ActBatch b{{codes}, {x}, {const_cast<void*>(scales)}, 1};
   return launched(launch_act8_unpack(b, d->format, d->rows, d->cols, d->ld, static_cast<hipStream_t>(stream)));
@@ -112,6 +157,10 @@ extern "C" int dcp_act8_gelu_bwd(const dcp_act8_desc* d, const void* codes, cons
   if (du == a) return fail(DCP_ERR_INVALID, "du and a are one buffer");
   const dcp_kept u{const_cast<void*>(codes), const_cast<void*>(scales)};
   DCP_TRY(check_kept(&u, d->format, "u"));
+  const bool wide = d->format == DCP_ACT_BF16;
+  DCP_TRY(apart({matrix(d, du, true), matrix(d, a, true), matrix(d, da, false),
+                 wide ? matrix(d, codes, false) : codes_of(d, codes, false),
+                 scales_of(d, wide ? nullptr : scales, false)}));
   DCP_TRY(check_device());
   return launched(launch_act_gelu_bwd(codes, scales, d->format, da, du, a, d->rows, d->cols, d->ld,
                                       static_cast<hipStream_t>(stream)));
@@ -135,6 +184,11 @@ extern "C" int dcp_gated_norm_fwd(const dcp_gated_norm_desc* d, const dcp_gated_
   if (y == out) return fail(DCP_ERR_INVALID, "out and y are one buffer");
   if (kf) DCP_TRY(check_kept(keep_f, d->keep_format, "keep_f"));
   if (ko) DCP_TRY(check_kept(keep_out, d->keep_format, "keep_out"));
+  const JoinBuffers b{d};
+  DCP_TRY(apart({b.written(out), b.written(y), b.row_scales(rstd_f, true), b.row_scales(rstd_out, true),
+                 b.data(kf ? keep_f : nullptr, true), b.scales(kf ? keep_f : nullptr, true),
+                 b.data(ko ? keep_out : nullptr, true), b.scales(ko ? keep_out : nullptr, true), b.read(x), b.read(f),
+                 b.weight(w->post, 1), b.weight(w->gate, b.gates()), b.weight(w->pre, 1), b.offsets()}));
   DCP_TRY(check_device());
   GatedNormFwd p{};
   p.x = x;
@@ -206,6 +260,15 @@ extern "C" int dcp_gated_norm_bwd(const dcp_gated_norm_desc* d, const dcp_gated_
   if (need > 0 && (!workspace || workspace_bytes < need || reinterpret_cast<uintptr_t>(workspace) % 256))
     return fail(DCP_ERR_WORKSPACE, "join backward workspace needs %zu bytes (256-byte aligned), got %zu", need,
                 workspace_bytes);
+  const JoinBuffers b{d};
+  Buffer dys = b.read(dy);
+  if (d->dy_f32) dys = {dy, Buffer::kRead, 4 * b.rows * b.h};
+  const dcp_kept *kf = need_f ? f : nullptr, *ko = w->pre ? out : nullptr;
+  DCP_TRY(apart({b.written(dx), b.written(df), b.written(y), b.grad(g->post, 1), b.grad(g->gate, b.gates()),
+                 b.grad(g->pre, 1), {workspace, Buffer::kWritten, need}, b.read(dout), dys, b.data(kf, false),
+                 b.scales(kf, false), b.data(ko, false), b.scales(ko, false),
+                 b.row_scales(w->post ? rstd_f : nullptr, false), b.row_scales(w->pre ? rstd_out : nullptr, false),
+                 b.weight(w->post, 1), b.weight(w->gate, b.gates()), b.weight(w->pre, 1), b.offsets()}));
   DCP_TRY(check_device());
   GatedNormBwd p{};
   p.dout = dout;
