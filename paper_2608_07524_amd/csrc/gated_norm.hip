@@ -620,11 +620,16 @@ constexpr int kFwdRowsMax = 4, kFwdTeams = 4096;
 hipError_t launch_gated_norm_fwd(const GatedNormFwd& p, hipStream_t s) {
   if (p.rows == 0) return hipSuccess;
   const int64_t want = p.rows / kFwdTeams;
-  const int team_rows = int(want < 1 ? 1 : want > kFwdRowsMax ? kFwdRowsMax : want);
+  int team_rows = int(want < 1 ? 1 : want > kFwdRowsMax ? kFwdRowsMax : want);
   with_lanes(team_lanes(p.hidden), [&](auto tl) {
     constexpr int TL = decltype(tl)::value;
-    const int64_t per_block = int64_t(Team<TL>::kTeams) * team_rows;
-    const dim3 grid(unsigned((p.rows + per_block - 1) / per_block)), block(Team<TL>::kBlock);
+    auto blocks = [&] {
+      const int64_t per_block = int64_t(Team<TL>::kTeams) * team_rows;
+      return (p.rows + per_block - 1) / per_block;
+    };
+    // (a launch holds fewer than 2^32 lanes: the last rows below 2^31 at a width of 64 or less)
+    while (blocks() * Team<TL>::kBlock >= int64_t(1) << 32) team_rows *= 2;
+    const dim3 grid{unsigned(blocks())}, block{unsigned(Team<TL>::kBlock)};
     if (!p.keep_f && !p.keep_out)
       hipLaunchKernelGGL((gated_norm_fwd_kernel<TL, DCP_ACT_BF16>), grid, block, 0, s, p, team_rows);
     else if (p.format == DCP_ACT_INT8)
