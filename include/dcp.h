@@ -525,7 +525,8 @@ int dcp_act8_gelu_bwd(const dcp_act8_desc* desc, const void* codes, const void* 
  *   rows            rows allocated in every matrix, in [0, 2^31).
  *   hidden          a positive multiple of 8, at most 4096 (DCP_ERR_UNSUPPORTED
  *                   beyond).
- *   n_seqs, cu_seqlens  a gate for each sequence: cu_seqlens is int32 [n_seqs+1]
+ *   n_seqs, cu_seqlens  a gate for each of at most 2^30 sequences (DCP_ERR_UNSUPPORTED
+ *                   beyond): cu_seqlens is int32 [n_seqs+1]
  *                   in DEVICE memory (cu[0] = 0, non-decreasing, cu[n_seqs] <= rows;
  *                   empty sequences are allowed), gate is [n_seqs, hidden], and rows
  *                   from cu[n_seqs] on are neither read for any output nor written.

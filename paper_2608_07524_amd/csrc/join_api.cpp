@@ -46,6 +46,7 @@ int check_join(const dcp_gated_norm_desc* d, const dcp_gated_norm_weights* w) {
     return fail(DCP_ERR_UNSUPPORTED, "hidden %d is not a multiple of 8 up to 4096", d->hidden);
   if (d->n_seqs < 0 || (d->n_seqs > 0) != (d->cu_seqlens != nullptr))
     return fail(DCP_ERR_INVALID, "n_seqs and cu_seqlens go together");
+  if (d->n_seqs > 1 << 30) return fail(DCP_ERR_UNSUPPORTED, "%d sequences: more than 2^30", d->n_seqs);
   if (reinterpret_cast<uintptr_t>(d->cu_seqlens) % 4) return fail(DCP_ERR_INVALID, "cu_seqlens is not 4-byte aligned");
   if (!std::isfinite(d->residual_scale)) return fail(DCP_ERR_INVALID, "residual_scale must be finite");
   if (!(std::isfinite(d->eps) && d->eps >= 0.f)) return fail(DCP_ERR_INVALID, "eps must be finite and >= 0");

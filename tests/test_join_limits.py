@@ -25,3 +25,17 @@ def test_join_of_almost_2_31_rows():
     c = P.gated_norm_bwd(x[-tail:], f=x[-tail:], rstd_f=s.rstd_f, post=g, gate=g, want_dx=False)
     assert torch.equal(b.df[-tail:], c.df)
     assert bool(torch.isfinite(b.dgate).all()) and bool(torch.isfinite(b.dpost).all())
+
+
+@pytest.mark.parametrize("n", [(1 << 30) + 1, (1 << 31) - 1])
+def test_join_of_too_many_sequences_is_refused(n):
+    """Beyond 2^30 the searches' and the launch's 32-bit counts would pass 2^31."""
+    lib, at, size = P.load(), 1 << 20, C.c_size_t()
+    d, w = N.GatedNormDescC(8, 64, n, at, 1.0, 1e-6, N.ACT_BF16, 0, 0), N.GatedNormPtrsC(None, 2 * at, None)
+    assert lib.dcp_gated_norm_bwd_workspace_size(d, size) == N.DCP_ERR_UNSUPPORTED and "sequences" in P.last_error()
+    assert lib.dcp_gated_norm_fwd(d, w, 3 * at, 4 * at, 5 * at, None, None, None, None, None,
+                                  None) == N.DCP_ERR_UNSUPPORTED
+    assert lib.dcp_gated_norm_bwd(d, w, 3 * at, None, N.KeptC(4 * at, None), None, None, None, None, 5 * at, None,
+                                  N.GatedNormPtrsC(None, 6 * at, None), 7 * at, 1 << 40, None) == N.DCP_ERR_UNSUPPORTED
+    ok = N.GatedNormDescC(8, 64, 1 << 30, at, 1.0, 1e-6, N.ACT_BF16, 0, 0)
+    assert lib.dcp_gated_norm_bwd_workspace_size(ok, size) == N.DCP_OK
