@@ -470,11 +470,11 @@ int dcp_layer_bwd(const dcp_layer_desc* desc, const dcp_layer_weights* w, const 
  * smallest integer >= -126 with max |x| <= qmax 2^k over the group, the byte is
  * k + 127, a code x / 2^k rounded to the format (nearest, ties to even), and the
  * value it stands for code 2^k, exact in bf16 (a value that was rounded up to
- * 2^128 reads back as infinity).  An element moves by at most half
- * a step: max |x| of its group / 127 (int8, whose scale wastes less than one
- * bit), or 2^-4 of itself (e4m3, from 2^-13 of the group's max on).  A group that
- * holds a NaN or an infinity reads back as NaN (byte 255, codes 0).  Codes are
- * [rows, cols] and scale bytes [rows, ceil(cols / 32)], both contiguous.
+ * 2^128 reads back as infinity).  An element moves by at most half a step: max |x| of
+ * its group / 127 (int8, whose scale wastes less than one bit; 2^-127 at the smallest
+ * scale, k = -126), or 2^-4 of itself (e4m3, from 2^-13 of the group's max on).  A
+ * group that holds a NaN or an infinity reads back as NaN (byte 255, codes 0).  Codes
+ * are [rows, cols] and scale bytes [rows, ceil(cols / 32)], both contiguous.
  */
 enum { DCP_ACT_BF16 = 0, DCP_ACT_INT8 = 1, DCP_ACT_E4M3 = 2 };
 
@@ -485,9 +485,10 @@ enum { DCP_ACT_BF16 = 0, DCP_ACT_INT8 = 1, DCP_ACT_E4M3 = 2 };
  *           >= cols (a slice of a wider matrix; columns outside are not touched).
  *   format  DCP_ACT_INT8 or DCP_ACT_E4M3 (DCP_ACT_BF16: dcp_act8_gelu_bwd only).
  * bf16 and fp32 pointers are 16-byte aligned, codes 8-byte.  The calls only
- * enqueue one kernel on `stream` (they may be captured into a graph).  A buffer that a
- * call of this section or the next writes may share no byte with another buffer of the
- * call, except as its description allows (DCP_ERR_INVALID).
+ * enqueue one kernel on `stream`, or one for every 2^34 elements (rows taken as whole
+ * groups) of larger matrices; they may be captured into a graph.  A buffer that a call of
+ * this section or the next writes may share no byte with another buffer of the call,
+ * except as its description allows (DCP_ERR_INVALID).
  */
 typedef struct {
   int64_t rows;
