@@ -159,17 +159,29 @@ struct Acts {
 };
 
 // W_up with GELU (and u's checkpoint) is one kernel of layer_proj.hip at every token
-// count, W_down^T with GELU' and GELU one where u is kept in bf16 and the layer's rule
-// takes it.  One kernel less the library's product and the passes behind it, us:
+// count.  One kernel less the library's product and the passes behind it, us:
 //   W_up, u in 8 bits  (128, 429) -18, (1152, 300) -4, (1152, 1000) -14, (1152, 4096)
 //              -23, (1152, 16381) -71, (1024, 16384) -36, (1536, 8192) -37, (1792,
 //              8192) +4, (4096, 4096) +47
 //   W_up, u in bf16    -16, -3, -13, -9, -20, -18, -11, +20, +72 (the rule is the same, so
 //              that the output does not depend on the stash)
-//   W_down^T, bf16     (256, 2048) -3, (1152, 1000) -3, (1152, 4096) -25, (1152, 16381)
-//              -36, (1024, 4096) +8, (1536, 8192) +4, (2048, 4096) +13
-//   W_down^T, 8 bits   -2, -2, -10, +29, +20, +34, +30: not taken
 inline bool fused_up(const Dims& d) { return d.h <= kProjHidden; }
+
+// W_down^T with GELU' and GELU is one kernel where u is kept in bf16 (8 bits: (1152, 16381)
+// +29, (1024, 4096) +20, (1536, 8192) +34) and the layer's rule for W_down^T with GELU'
+// takes it, but for multiples of 256 from 1,024 on, which suit the library's tiles: there up
+// to 12 M elements of a [T, hidden] matrix, and, where 192-wide tiles pad the width by a tenth
+// (1,024), 1 M.  One kernel less the library's product and the pass, us, at 1,000 / 2,048 /
+// 4,096 / 8,192 / 12,288 / 16,384 / 24,576 tokens:
+//   256   -11 / -10 / -6 / -1 / -5 / -2 / -3        576   -6 / -1 / -4 / -19 / -2 / -11 / -6
+//   768   -3 / -3 / -8 / -7 / -2 / +1 / -21         1,152 -0 / -0 / -16 / -8 / -12 / -33 / +3
+//   1,408 -4 / -12 / +1 / -14 / -36 / +3 / +12      1,024 +1 / +2 / +8 / +9 / +14 / +15 / +29
+//   1,280 -4 / -5 / -7 / -27 / +13 / +21 / +50      1,536 -2 / -5 / -3 / +7 / -27 / +13 / +24
+inline bool fused_back(const Dims& d) {
+  const bool padded = 10 * kProjTile * proj_tiles(d.h) > 11 * d.h;
+  const bool library = d.h % 256 == 0 && d.h >= 1024 && d.T * d.h > int64_t(padded ? 1 : 12) << 20;
+  return fused_gelu(d) && !library;
+}
 
 // Activations in bf16 at `base`, in kept_layout's places; f1 and f2, where it has
 // none, behind them.
@@ -432,7 +444,7 @@ extern "C" int dcp_block_bwd(const dcp_block_desc* desc, const dcp_block_weights
   }
   // MLP: dA = dF2 Wdown^T; dU = dA GELU'(U) in place, A = GELU(U)
   void* da = at(workspace, v.da);
-  if (format == DCP_ACT_BF16 && fused_gelu(d)) {
+  if (format == DCP_ACT_BF16 && fused_back(d)) {
     const Proj p{{df2}, {lw.w_down}, {da}, s.bf16[kU], a, T, int(4 * h), int(h), 1, 1, 0, format, nullptr};
     DCP_HIP(launch_proj(p, ProjEpilogue::kGeluBack, st));
   } else {
