@@ -271,13 +271,20 @@ inline BwdShape bwd_shape(int64_t rows, int hidden, int n_seqs) {
   s.teams_of_block = s.block / s.lanes;
   // Rows of a team: the workgroups are one evenly filled round of what fits the chip, or
   // as few as teams of at most kBwdRowsMax rows (which a lane adds one after another)
-  // allow; two where sequences are short, whose ends cost a team as much as a row and are
-  // not spread evenly, if that leaves a team four rows (65,536 rows of 64: three rows a
-  // team 35 us, two 44).  Long sequences, 131,072 rows of hidden 1,152: 103 / 64 / 52 / 32 /
-  // 16 rows 392 / 411 / 401 / 409 / 429 us; 16,384 rows of 4,096: 64 / 32 / 16 / 8 rows 192
-  // / 197 / 202 / 208.  Sequences of 1 to 51 rows, one round / two: on average 17 to 23
-  // rows, 30,000 rows of 2,048 214 / 192, 16,384 of 4,096 249 / 228, 65,536 of 576 144 /
-  // 126, of 1,152 252 / 226; on average 51, 65,536 of 1,152 211 / 219.
+  // allow.  Long sequences, 131,072 rows of hidden 1,152: 103 / 64 / 52 / 32 / 16 rows
+  // 392 / 411 / 401 / 409 / 429 us; 16,384 rows of 4,096: 64 / 32 / 16 / 8 rows 192 / 197
+  // / 202 / 208.
+  //   Two rounds where sequences have fewer than kShortRows rows on average, if that
+  // leaves a team four rows (65,536 rows of 64: three rows a team 35 us, two 44).  A
+  // sequence's end costs a team as much as a row, and clips of one frame beside longer ones
+  // put many ends into few teams, which a second round evens out.  The host knows no more of
+  // that than the average (allocated rows, all sequences, empty ones too).  One round / two:
+  //   clips of 1, 16, 32 or 51 rows mixed, average 16 to 20: 131,072 rows of 1,152 503 to
+  //     528 / 412 to 476, of 256 129 to 134 / 110 to 134; 32,768 of 4,096, 7: 470 / 413
+  //   average 32 to 50, nothing in sum: of 1,152 34 rows 397 / 408, 35 398 / 423, 39 500 /
+  //     414, 42 398 / 405, 49 395 / 406, 51 395 / 404; of 2,048 32 rows 183 / 192, 36 206 / 190
+  //   lengths uniform from 1 to twice the average, where ends are spread evenly: 2 to 6 %
+  //     lost at any average (of 1,152: 16 rows 408 / 420, 32 402 / 414, 64 396 / 406)
   const int64_t round = int64_t(s.teams_of_block) * kNumCU * (4 * bwd_waves(s.lanes) / (s.block / 64));
   const bool shorts = n_seqs > 0 && rows < int64_t(kShortRows) * n_seqs && rows >= 8 * round;
   const int64_t least = (rows + round * kBwdRowsMax - 1) / (round * kBwdRowsMax);
