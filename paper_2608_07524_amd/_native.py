@@ -624,9 +624,10 @@ class Layer:
 
 def _enqueue(torch, device, fn, *args):
     """fn(*args, current stream of ``device``), with ``device`` as the current one."""
-    # (the raw handle: torch.cuda.current_stream builds an object, 2 us a call)
-    stream = torch._C._cuda_getCurrentRawStream(device.index)
-    if device.index == torch._C._cuda_getDevice():
+    # (the raw handle where this torch has it: current_stream builds an object, 2 us a call)
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    stream = raw(device.index) if raw else torch.cuda.current_stream(device).cuda_stream
+    if device.index == torch.cuda.current_device():
         st = fn(*args, stream)
     else:
         with torch.cuda.device(device):

@@ -1,0 +1,31 @@
+"""The binding of joins and checkpoints without a GPU: the stream that a call is given, and
+the size of a join's workspace."""
+
+import contextlib
+import ctypes as C
+import types
+
+import pytest
+
+import paper_2608_07524_amd as P
+from paper_2608_07524_amd import _native as N
+
+
+@pytest.mark.parametrize("raw", [True, False])
+@pytest.mark.parametrize("current", [0, 1])
+def test_calls_follow_the_current_stream_of_the_tensors_device(raw, current):
+    """With and without the raw handles that some builds of torch offer."""
+    entered = []
+
+    @contextlib.contextmanager
+    def device(d):
+        entered.append(d.index)
+        yield
+
+    cuda = types.SimpleNamespace(current_device=lambda: current, device=device,
+                                 current_stream=lambda d: types.SimpleNamespace(cuda_stream=100 + d.index))
+    private = types.SimpleNamespace(_cuda_getCurrentRawStream=lambda i: 100 + i) if raw else types.SimpleNamespace()
+    calls = []
+    N._enqueue(types.SimpleNamespace(cuda=cuda, _C=private), types.SimpleNamespace(index=1),
+               lambda *a: calls.append(a) or N.DCP_OK, 7)
+    assert calls == [(7, 101)] and entered == ([] if current == 1 else [1])
