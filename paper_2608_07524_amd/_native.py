@@ -624,10 +624,12 @@ class Layer:
 
 def _enqueue(torch, device, fn, *args):
     """fn(*args, current stream of ``device``), with ``device`` as the current one."""
-    # (the raw handle where this torch has it: current_stream builds an object, 2 us a call)
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    stream = raw(device.index) if raw else torch.cuda.current_stream(device).cuda_stream
-    if device.index == torch.cuda.current_device():
+    # (the raw handles where this torch has them: the public calls take 2 us more)
+    try:
+        stream, current = torch._C._cuda_getCurrentRawStream(device.index), torch._C._cuda_getDevice()
+    except AttributeError:
+        stream, current = torch.cuda.current_stream(device).cuda_stream, torch.cuda.current_device()
+    if device.index == current:
         st = fn(*args, stream)
     else:
         with torch.cuda.device(device):

@@ -24,7 +24,9 @@ def test_calls_follow_the_current_stream_of_the_tensors_device(raw, current):
 
     cuda = types.SimpleNamespace(current_device=lambda: current, device=device,
                                  current_stream=lambda d: types.SimpleNamespace(cuda_stream=100 + d.index))
-    private = types.SimpleNamespace(_cuda_getCurrentRawStream=lambda i: 100 + i) if raw else types.SimpleNamespace()
+    private = types.SimpleNamespace()
+    if raw:
+        private._cuda_getCurrentRawStream, private._cuda_getDevice = lambda i: 100 + i, lambda: current
     calls = []
     N._enqueue(types.SimpleNamespace(cuda=cuda, _C=private), types.SimpleNamespace(index=1),
                lambda *a: calls.append(a) or N.DCP_OK, 7)
