@@ -867,6 +867,16 @@ def _kept(torch, name, t, shape, device):
     return ACT_BF16, KeptC(t.data_ptr(), None)
 
 
+def gated_norm_bwd_workspace_size(rows: int, hidden: int, n_seqs: int = 0) -> int:
+    """Bytes of gated_norm_bwd's ``workspace`` for [rows, hidden] and, with
+    ``cu_seqlens``, ``n_seqs`` sequences."""
+    unread = C.c_int32()  # (the size depends on the number of offsets only)
+    d = GatedNormDescC(rows, hidden, n_seqs, C.addressof(unread) if n_seqs else None, 1.0, 0.0, ACT_BF16, 0, 0)
+    n = C.c_size_t()
+    _check(load().dcp_gated_norm_bwd_workspace_size(d, n))
+    return n.value
+
+
 def gated_norm_bwd(dout, dy=None, f=None, out=None, rstd_f=None, rstd_out=None, post=None, gate=None, pre=None,
                    cu_seqlens=None, residual_scale: float = 1.0, want_y: bool = False, want_dx: bool = True, dx=None,
                    df=None, y=None, workspace=None) -> GatedNormGrads:
@@ -874,7 +884,8 @@ def gated_norm_bwd(dout, dy=None, f=None, out=None, rstd_f=None, rstd_out=None, 
     activations in bf16, or their checkpoints (codes, scales), in one format;
     ``dy`` bf16 or float32; ``dout`` may be None (zero) where ``pre`` is given;
     ``want_y`` returns y again, formed from ``out`` as kept.  Rows behind the last
-    sequence are left as they are."""
+    sequence are left as they are.  ``workspace``: gated_norm_bwd_workspace_size bytes,
+    256-byte aligned; calls that may overlap in time need one each."""
     import torch
     ref = dout if dout is not None else dy
     if not isinstance(ref, torch.Tensor) or ref.dim() != 2:

@@ -88,3 +88,22 @@ def test_checkpoints_beside_each_other(torch, P):
     wide = torch.cat([x, x], 1)
     back = P.act8_unpack(*want, out=wide[:, cols:])
     assert torch.equal(back, P.act8_unpack(*want)) and torch.equal(wide[:, :cols], x)
+
+
+def test_workspace_of_the_stated_size(torch, P):
+    """gated_norm_bwd_workspace_size is enough, nothing behind it is written, and a byte less
+    is refused."""
+    rng = np.random.default_rng(3)
+    rows, h, cu = 5000, 1152, [0, 7, 7, 2000, 2003, 4990]
+    g, gate = _rand(torch, rng, h), _rand(torch, rng, len(cu) - 1, h)
+    x, f, dout = (_rand(torch, rng, rows, h) for _ in range(3))
+    r = P.gated_norm_fwd(x, f, g, gate, g, cu)
+    back = lambda **kw: P.gated_norm_bwd(dout, dout, f, r.out, r.rstd_f, r.rstd_out, g, gate, g, cu, **kw)
+    size = P.gated_norm_bwd_workspace_size(rows, h, len(cu) - 1)
+    room = torch.full((size + 256,), 255, dtype=torch.uint8, device="cuda")
+    got, want = back(workspace=room[:size]), back()
+    for name in ("dpost", "dgate", "dpre"):
+        assert torch.equal(getattr(got, name), getattr(want, name)), name
+    assert bool((room[size:] == 255).all())
+    with pytest.raises(P.DCPError, match="workspace"):
+        back(workspace=room[:size - 1])
