@@ -9,9 +9,10 @@
 // code 2^k.  Powers of two make both directions exact but for that one rounding:
 // x 2^-k and code 2^k are exact in fp32 and code 2^k is exact in bf16 (2^128, to
 // which values next to it round, is infinity there), so a checkpoint is the same
-// bits wherever it is made, and reading it back in bf16 loses nothing.  (A scale that is not a power of two would use the range of int8
-// better, by 0.4 bit on average, and round twice.)  A group that holds a NaN or an
-// infinity gets byte 255 and codes 0, which read back as NaN.
+// bits wherever it is made, and reading it back in bf16 loses nothing.  (A scale that
+// is not a power of two would use the range of int8 better, by 0.4 bit on average, and
+// round twice.)  A group that holds a NaN or an infinity gets byte 255 and codes 0,
+// which read back as NaN.
 #pragma once
 
 #include <hip/hip_runtime.h>

@@ -16,3 +16,10 @@ int fail(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
 void clear_error();
 
 }  // namespace dcp
+
+// Returns from the calling function with x's status unless that is DCP_OK.
+#define DCP_TRY(x)       \
+  do {                   \
+    int st_ = (x);       \
+    if (st_) return st_; \
+  } while (0)

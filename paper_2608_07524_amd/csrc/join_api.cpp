@@ -117,12 +117,6 @@ int check_kept(const dcp_kept* k, int format, const char* what) {
 
 using namespace dcp;
 
-#define DCP_TRY(x)       \
-  do {                   \
-    int st_ = (x);       \
-    if (st_) return st_; \
-  } while (0)
-
 extern "C" int dcp_act8_pack(const dcp_act8_desc* d, const void* x, void* codes, void* scales, void* stream) {
   clear_error();
   DCP_TRY(check_act8(d, false));

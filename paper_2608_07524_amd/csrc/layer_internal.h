@@ -98,11 +98,6 @@ inline bool library_wgrad(const Dims& d) { return d.h >= 4096 && d.T >= 12288; }
 
 inline char* at(void* base, size_t off) { return static_cast<char*>(base) + off; }
 
-#define DCP_TRY(x)          \
-  do {                      \
-    int st_ = (x);          \
-    if (st_) return st_;    \
-  } while (0)
 #define DCP_HIP(x)                                                                          \
   do {                                                                                      \
     hipError_t e_ = (x);                                                                    \

@@ -324,7 +324,8 @@ __global__ __launch_bounds__(kThreads, 2) void proj_kernel(Proj p) {
           // (a group's four lanes have one row and N is a multiple of 32: all or none are here)
           const uint32_t byte = scale_byte<FMT>(group_top(top_bits(r)));
           *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(p.out[0]) + at) = encode8<FMT>(r, byte);
-          if (c % 4 == 0) static_cast<uint8_t*>(p.scales)[int64_t(row) * (N / kActGroup) + col / kActGroup] = uint8_t(byte);
+          uint8_t* scales = static_cast<uint8_t*>(p.scales) + int64_t(row) * (N / kActGroup);
+          if (c % 4 == 0) scales[col / kActGroup] = uint8_t(byte);
         } else {
           *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.out[pl.out]) + at) = r;
         }
