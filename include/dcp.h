@@ -627,7 +627,9 @@ int dcp_gated_norm_bwd(const dcp_gated_norm_desc* desc, const dcp_gated_norm_wei
  * outputs, in stash_format (see dcp_act8_desc), o in bf16 (its gradient's row sums have
  * to cancel), and the LSE and row scales in fp32: 9 or 11 elements a token and hidden
  * column, where the layer's stash holds 15 in bf16 (y1, y2 and a are formed again in
- * the backward).  An 8-bit stash changes the gradients by its rounding, not the output:
+ * the backward: y2 from h as held, the forward's from h in fp32, and a = GELU(u) in
+ * another order of the same fp32 operations, so that either may differ from the
+ * forward's by a rounding to bf16).  An 8-bit stash changes the gradients by its rounding, not the output:
  * the attention's weights, for one, are formed again from q and k as held against the
  * LSE of the forward, each off by the factor e^(what its logit moved), so that large
  * logits want int8.  A recomputing backward (stash NULL) forms everything again in bf16.

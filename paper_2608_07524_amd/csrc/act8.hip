@@ -4,7 +4,8 @@
 // reads 3 + 1/32 and writes 4.  One 16-byte access of the bf16 side a lane, eight
 // elements, so that four lanes hold a group and its largest magnitude takes two lane
 // moves.  16,381 x 4,608 in int8: pack 41 us (5.6 TB/s), unpack 33 (7.0: the codes
-// come from the last-level cache), GELU backward 88 (6.0); a 2 GiB copy 4.92 TB/s.
+// come from the last-level cache), GELU backward 88 (6.0), from a bf16 u 103 (5.9); a
+// 2 GiB copy 4.9 to 5.0 TB/s.
 // 429 x 256: 2.5 us each, the launch.
 #include "act8.h"
 #include "block_launch.h"

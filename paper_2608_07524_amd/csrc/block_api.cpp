@@ -12,6 +12,12 @@
 // it), and packs q, k and v in one launch; the backward's joins and activation read
 // theirs in place, and one launch brings q, k and v back for the attention.
 //
+// The weight gradients of W_up and W_down multiply y2 and a as formed again: y2 from h as
+// held (the forward's comes from h in fp32), a by gelu_and_slope (act8.h; the forward's by
+// the gelu of layer_proj.hip or layer.hip: the same function in another order of fp32
+// operations).  With a bf16 stash either is within a rounding to bf16, 2^-8 of itself, of
+// what the forward multiplied, as far as any bf16 product's operands are known.
+//
 // o stays in bf16 in every stash.  The backward forms Delta = dO . o, which the sum over
 // keys of P (dO . v) has to cancel: o's rounding does not (v's averages out over the
 // keys), and the difference, the same for all keys of a query, becomes a part of dQ that

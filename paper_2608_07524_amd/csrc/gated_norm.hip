@@ -13,10 +13,11 @@
 // HBM-bound: every input is read once and every output written once, all of a row
 // in registers between; sums, statistics and gradients of the parameters are fp32.
 // 131,072 rows of hidden 1,152, eight sequences, int8: join with f's checkpoint 257
-// us (5.3 TB/s), backward 384 + 12 (4.7 TB/s, and the partial rows), a 2 GiB copy 4.92
-// TB/s.  65,536 rows in 1,286 sequences of 1 to 51 tokens: 198 + 12.  16,384 rows of
-// hidden 4,096 in bf16: join 98 (5.5), backward 190 + 5 (4.9).  429 rows of 256: 3.7;
-// 5.6 + 5.7, chains of memory latencies.
+// us (5.3 TB/s), with f's and out's, as a block's first join, 281 (5.4); backward 384 + 12
+// (4.7 TB/s, and the partial rows), with fp32 dy, as in a block, 450 in all (4.7); a 2 GiB
+// copy 4.9 to 5.0 TB/s.  65,536 rows in 1,286 sequences of 1 to 51 tokens: 198 + 12.
+// 16,384 rows of hidden 4,096 in bf16: join 98 (5.5), backward 190 + 5 (4.9).  429 rows of
+// 256: 3.7; 5.6 + 5.7, chains of memory latencies.
 #include <type_traits>
 
 #include "act8.h"
@@ -261,7 +262,10 @@ inline int team_lanes(int hidden) {
   return l;
 }
 // Wavefronts that share a SIMD: 128 registers each where a team's rows and offsets are in
-// scalar registers, more otherwise.
+// scalar registers, more otherwise.  2 to 6 of the 128 spill at 448 and 512 lanes with an
+// fp32 dy (bf16 activations: from 384 lanes) and 2 at 512 with a bf16 dy and int8, at no
+// cost that shows: 32,768 rows of 4,096, int8, 390 us with fp32 dy and 341 with bf16, 2,048
+// wide (no spills) 60,000 rows 373 and 325, all 4.7 to 4.8 TB/s.
 constexpr int bwd_waves(int lanes) { return lanes < 64 ? 3 : 4; }
 constexpr int kBwdRowsMax = 128, kShortRows = 32;
 inline BwdShape bwd_shape(int64_t rows, int hidden, int n_seqs) {
