@@ -265,7 +265,7 @@ inline int team_lanes(int hidden) {
 // scalar registers, more otherwise.  2 to 6 of the 128 spill at 448 and 512 lanes with an
 // fp32 dy (bf16 activations: from 384 lanes) and 2 at 512 with a bf16 dy and int8, at no
 // cost that shows: 32,768 rows of 4,096, int8, 390 us with fp32 dy and 341 with bf16, 2,048
-// wide (no spills) 60,000 rows 373 and 325, all 4.7 to 4.8 TB/s.
+// wide (no spills) 60,000 rows 373 and 325, all 4.6 to 4.8 TB/s.
 constexpr int bwd_waves(int lanes) { return lanes < 64 ? 3 : 4; }
 constexpr int kBwdRowsMax = 128, kShortRows = 32;
 inline BwdShape bwd_shape(int64_t rows, int hidden, int n_seqs) {
